@@ -82,7 +82,10 @@ enum {
   SAAP_OP_BUCKET_ATTENTION_MASS_BATCH = 10,  /* shape: S, Hkv, N = queries per KV head, B */
   SAAP_OP_PLANNED_DECODE_ATTENTION = 11,     /* shape: S, Hq, Hkv, mode */
   SAAP_OP_PREFILL_SPARSE_ATTENTION = 12,     /* shape: S, Hq, Hkv, N = query tokens per sequence (Tq), nprobe, dtype */
-  SAAP_OP_UPDATE_CENTROIDS_FROM_IDS = 13     /* shape: S, Hkv, N, B */
+  SAAP_OP_UPDATE_CENTROIDS_FROM_IDS = 13,    /* shape: S, Hkv, N, B */
+  SAAP_OP_NORM_ROTATE_GRADS = 14,            /* shape: S, Hq, Hkv (0: a tensor that is not given), N = tokens per sequence (T) */
+  SAAP_OP_TREE_DECODE_ATTENTION = 15         /* shape: S, Hq, Hkv, N = tokens per tree (T), B = runs (0: dense cache), nprobe,
+                                                mode = 1 if every token has its own list, dtype = SAAP_F32 for an fp32 cache */
 };
 
 #define SAAP_WS_HEADER_BYTES 65536u
@@ -827,6 +830,145 @@ int32_t saap_window_push_fp8(const void* x_new, const void* k_new, const void* v
                              int32_t S, int32_t Hkv, int32_t Ncap, int32_t B, int32_t d,
                              int32_t n_sink, int32_t n_recent,
                              void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ---- drafted tokens ----
+ * A program that drafts several tokens ahead of the model decodes them together, as a tree, and keeps the branch that the
+ * model agrees with.  The calls below are what that takes around the bucketed cache, in the order of their use; single-token
+ * decoding and prompts are their smallest and largest cases.
+ *
+ * norm_rotate -- from a projection's queries and keys to what the other calls take: the norm over the features of every head,
+ * and the rotation by the token's position.  Section 4 ("Assigning with(out) RoPE"): buckets and query model work on the
+ * features BEFORE the rotation, the attention on those after it, so both come out of one pass.
+ *   y = x / sqrt(mean(x^2) + eps) * weight      (norm = 0: y = x)                                    -> features
+ *   rotated = y with pair i of its first `rot` features, i < rot / 2, turned by the angle positions[s,t] * freqs[i] and
+ *             multiplied by `magnitude`:  (a, b) -> magnitude (a cos - b sin, b cos + a sin)         -> rotated
+ *             pairs = 0: features i and i + rot/2;  pairs = 1: features 2i and 2i + 1
+ *   The features from `rot` on are passed on as they are (not multiplied).
+ *   q [S,T,Hq,d], k [S,T,Hkv,d] dtype, tokens q_stride and k_stride elements apart (at least Hq*d, Hkv*d; a multiple of 16
+ *     bytes), so that slices of one projection's output can be given; either may be NULL
+ *   positions [S,T] int32; freqs [rot/2] DOUBLE (device), in radians per position: the product is taken and reduced in double
+ *     precision, so that any position is turned as exactly as the first
+ *   q_weight, k_weight fp32 [d], or [Hq,d] and [Hkv,d] with weight_per_head = 1; or NULL (all ones; NULL if norm = 0)
+ *   q_feat, q_rot [S,T,Hq,d] dtype, out (token-major, as the decode calls take queries);
+ *   k_feat, k_rot [S,Hkv,T,d] dtype, out (head-major, as assign_keys, build_bucket_index and the trees take keys)
+ *   Of the two outputs of a given tensor either may be NULL.  Outputs must not overlap inputs.
+ * rot is a multiple of 16 up to d.  Sums, angles and products are in fp32 (angles' reduction in fp64), rounded once.
+ */
+typedef struct {
+  const int32_t* positions;
+  const double* freqs;
+  const float* q_weight;
+  const float* k_weight;
+  int64_t q_stride, k_stride;
+  int32_t S, T, Hq, Hkv, d, rot, pairs, norm, weight_per_head, dtype;
+  float eps, magnitude;
+} saap_rotation;   /* host struct of device pointers and sizes */
+
+int32_t saap_norm_rotate(const saap_rotation* rotation /* host */, const void* q, const void* k,
+                         void* q_feat, void* q_rot, void* k_feat, void* k_rot, void* stream);
+
+/*
+ * norm_rotate_grads -- the gradients of saap_norm_rotate from those of its outputs:
+ *   g = g_feat + (the rotation turned back, times magnitude) g_rot
+ *   dweight = sum over the rows of a weight row of  g * n,  n = x / sqrt(mean(x^2) + eps)
+ *   dx = (u - n mean(u n)) / sqrt(mean(x^2) + eps),  u = g * weight      (norm = 0: dx = g)
+ *   g_q_feat, g_q_rot, g_k_feat, g_k_rot: shaped as the outputs; of a given tensor either may be NULL (zero), not both
+ *   dq [S,T,Hq,d], dk [S,T,Hkv,d] dtype, out, dense; dq_weight, dk_weight fp32, out, given if and only if the weight is
+ * The weights' sums run in fp32 in a fixed order: the same inputs give the same bits.
+ * Workspace: SAAP_OP_NORM_ROTATE_GRADS (may be NULL where no weight's gradient is asked for).
+ */
+int32_t saap_norm_rotate_grads(const saap_rotation* rotation /* host */, const void* q, const void* k,
+                               const void* g_q_feat, const void* g_q_rot, const void* g_k_feat, const void* g_k_rot,
+                               void* dq, void* dk, float* dq_weight, float* dk_weight,
+                               void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * tree_decode_attention -- saap_sparse_decode_attention / saap_windowed_decode_attention for T tokens of every sequence at once
+ * (1 <= T <= 64), each over the members of its listed buckets and over those of the T drafted keys that the tree says:
+ *   the row (token t, query head) of sequence s attends, of KV head h,
+ *     the members n of the runs in its list, and of resident_run (-1: none), with position(n) >= starts[s,t];
+ *     the drafted keys j < T with bit j of tree[s,t] set (a token's own key is attended if its own bit is)
+ *   a_n = scale <q, k_n>;  softcap > 0: a_n <- softcap tanh(a_n / softcap);  slopes: a_n <- a_n - slopes[hq] (pos[s,t] - position(n))
+ *   out = sum_n softmax(a)_n v_n,  lse = log sum_n exp(a_n);  a row that attends nothing: out = 0, lse = -inf
+ *   q [S,T,Hq,d] dtype;  k_tree, v_tree [S,Hkv,T,d] dtype (what saap_norm_rotate writes) and tree [S,T] 64-bit masks: all three,
+ *     or all NULL (the cache alone).  What keys and values hold that no row attends does not matter.  A padded batch gives the
+ *     tokens that are not there a mask of 0.
+ *   selected [S,Hkv,nprobe]: one list for the tokens of a tree (lists_per_token = 0), or [S,T,Hkv,nprobe]: a list per token
+ *     (lists_per_token = 1; what saap_select_buckets writes for S*T sequences), which gives every drafted token the result of
+ *     decoding it alone.  Ids outside [0,runs) are passed over, one listed twice counts once.
+ *     The union of a tree's lists is read once.
+ *   off [S,Hkv,runs+1], len [S,Hkv,runs], idx [S,Hkv,Ncap] as saap_build_bucket_index or saap_build_windowed_index wrote them;
+ *     idx gives the positions, and is needed for slopes or starts
+ *   slopes [Hq] fp32 or NULL; pos [S,T] int32: the tokens' positions, also those of the drafted keys (NULL without slopes);
+ *   starts [S,T] int32 or NULL: the first position that a token attends (the begin of its document, or of its span)
+ *   out [S,T,Hq,d] of out_dtype;  lse [S,T,Hq] fp32 or NULL
+ * G in {1,2,4,8}; S*Hkv <= 4096; Ncap < 2^23; B <= SAAP_MAX_BUCKETS.
+ * Arithmetic: products of bf16 values are summed in fp32 by the matrix cores; softmax and its sums are in fp32; a weight enters
+ * the product with the values in full where out is fp32, with 16 significant bits where it is bf16.  The same inputs give the
+ * same bits on the same device.
+ * Workspace: SAAP_OP_TREE_DECODE_ATTENTION.
+ */
+typedef struct {
+  const int64_t* tree;
+  const void* k_tree;
+  const void* v_tree;
+  const int32_t* idx;
+  const float* slopes;
+  const int32_t* pos;
+  const int32_t* starts;
+  int32_t S, T, Hq, Hkv, d;
+  float scale, softcap;
+} saap_tree;   /* host struct of device pointers and sizes; a field that a call does not need is NULL or 0 */
+
+int32_t saap_tree_decode_attention(const saap_tree* tree /* host */, const void* q, const void* Ksorted, const void* Vsorted,
+                                   const int32_t* off, const int32_t* len, const int32_t* selected, int32_t nprobe,
+                                   int32_t lists_per_token, int32_t resident_run, void* out, int32_t out_dtype, float* lse,
+                                   int32_t Ncap, int32_t runs, int32_t dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* The same on an 8-bit cache written by saap_quantize_kv (q, k_tree, v_tree bf16). */
+int32_t saap_tree_decode_attention_fp8(const saap_tree* tree /* host */, const void* q, const uint8_t* K8, const uint8_t* V8,
+                                       const float* kscale, const float* vscale,
+                                       const int32_t* off, const int32_t* len, const int32_t* selected, int32_t nprobe,
+                                       int32_t lists_per_token, int32_t resident_run, void* out, int32_t out_dtype, float* lse,
+                                       int32_t Ncap, int32_t runs, void* ws, size_t ws_bytes, void* stream);
+
+/* The same over every key of a packed cache K, V [S,Hkv,N,d] in position order (position(n) = n; idx is not used):
+ * n_keys [S] int32 (device) or NULL: how many of the N rows a sequence holds (0 .. N; values outside are cut). */
+int32_t saap_dense_tree_decode_attention(const saap_tree* tree /* host */, const void* q, const void* K, const void* V,
+                                         const int32_t* n_keys, void* out, int32_t out_dtype, float* lse,
+                                         int32_t N, int32_t dtype, void* ws, size_t ws_bytes, void* stream);
+
+int32_t saap_dense_tree_decode_attention_fp8(const saap_tree* tree /* host */, const void* q, const uint8_t* K8,
+                                             const uint8_t* V8, const float* kscale, const float* vscale,
+                                             const int32_t* n_keys, void* out, int32_t out_dtype, float* lse,
+                                             int32_t N, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * append_accepted -- the drafted tokens that are kept join the cache, as many of every sequence as its path says, in one call:
+ * the index ends up as saap_append_keys, called for one token after the other, would leave it (resident_ids != NULL:
+ * saap_window_push).  Their buckets are given (saap_assign_keys on the drafted features).
+ *   bucket_ids [S,Hkv,T] int32; k_tree, v_tree [S,Hkv,T,d] dtype: of all drafted tokens
+ *   path [S,P] int32: the accepted ones in the order of their positions; an entry outside [0,T) ends a path; 0 < P <= 64
+ *   pos_new [S] int32: position of a path's first token, the others follow (NULL records -2; not with resident_ids)
+ *   off, len, idx, Ksorted, Vsorted, overflow_flag as in saap_append_keys: a key whose bucket is full, or whose id is outside
+ *     [0,B), is not stored and sets the flag, the others are stored
+ *   resident_ids [S,Hkv,W], n_sink, n_recent: the index of saap_build_windowed_index (B + 1 runs); a push that is refused
+ *     leaves its ring slot as it was.  P <= n_recent, unless n_recent = 0.  NULL, 0, 0: an index without a window (B runs).
+ */
+int32_t saap_append_accepted(const int32_t* bucket_ids, const void* k_tree, const void* v_tree, const int32_t* path,
+                             const int32_t* pos_new, const int32_t* off, int32_t* len, int32_t* idx,
+                             void* Ksorted, void* Vsorted, int32_t* resident_ids, int32_t* overflow_flag,
+                             int32_t S, int32_t Hkv, int32_t T, int32_t P, int32_t Ncap, int32_t B, int32_t d, int32_t dtype,
+                             int32_t n_sink, int32_t n_recent, void* stream);
+
+/* The same on an 8-bit cache: k_tree, v_tree bf16, stored as saap_append_keys_fp8 stores them. */
+int32_t saap_append_accepted_fp8(const int32_t* bucket_ids, const void* k_tree, const void* v_tree, const int32_t* path,
+                                 const int32_t* pos_new, const int32_t* off, int32_t* len, int32_t* idx,
+                                 uint8_t* K8, uint8_t* V8, const float* kscale, const float* vscale,
+                                 int32_t* resident_ids, int32_t* overflow_flag,
+                                 int32_t S, int32_t Hkv, int32_t T, int32_t P, int32_t Ncap, int32_t B, int32_t d,
+                                 int32_t n_sink, int32_t n_recent, void* stream);
 
 #ifdef __cplusplus
 }

@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes
 import importlib
+import math
 import os
 
 import torch
@@ -23,6 +24,7 @@ OP_ASSIGN_KEYS, OP_BUILD_BUCKET_INDEX, OP_CLASSIFY_QUERIES, OP_SELECT_BUCKETS = 
 OP_SPARSE_DECODE_ATTENTION, OP_DENSE_DECODE_ATTENTION, OP_APPEND_KEYS, OP_WINDOW_PUSH = 4, 5, 6, 7
 OP_BUCKET_ATTENTION_MASS, OP_QUERY_MODEL_LOSS_GRADS, OP_BUCKET_ATTENTION_MASS_BATCH = 8, 9, 10
 OP_PLANNED_DECODE_ATTENTION, OP_PREFILL_SPARSE_ATTENTION, OP_UPDATE_CENTROIDS_FROM_IDS = 11, 12, 13
+OP_NORM_ROTATE_GRADS, OP_TREE_DECODE_ATTENTION = 14, 15
 WS_HEADER_BYTES = 65536
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -38,6 +40,8 @@ NATIVE = (
     "dense_decode_attention", "dense_decode_attention_fp8", "select_attend", "select_attend_fp8",
     "planned_decode_attention", "planned_decode_attention_fp8", "prefill_sparse_attention",
     "append_keys", "append_keys_fp8", "window_push", "window_push_fp8", "adam_update",
+    "norm_rotate", "norm_rotate_grads", "tree_decode_attention", "tree_decode_attention_fp8",
+    "dense_tree_decode_attention", "dense_tree_decode_attention_fp8", "append_accepted", "append_accepted_fp8",
 )
 
 EXPORTS = (
@@ -56,6 +60,8 @@ EXPORTS = (
     "saap_prefill_sparse_attention", "saap_classify_select", "saap_select_attend", "saap_select_attend_fp8", "saap_select_attend_windowed",
     "saap_build_bucket_index_zeroed", "saap_build_windowed_index_zeroed",
     "saap_update_centroids_from_ids",
+    "saap_norm_rotate", "saap_norm_rotate_grads", "saap_tree_decode_attention", "saap_tree_decode_attention_fp8",
+    "saap_dense_tree_decode_attention", "saap_dense_tree_decode_attention_fp8", "saap_append_accepted", "saap_append_accepted_fp8",
 )
 
 
@@ -428,6 +434,49 @@ def lloyd_iterations(x, centroids, iters, normalize=True):
     return c
 
 
+def rotary_frequencies(rot, theta=500000.0, scaling=None, factor=1.0, context=8192, low=1.0, high=4.0, device="cuda"):
+    """Radians per position of the rot/2 pairs that norm_rotate turns, float64: theta^(-2i/rot), scaled for contexts `factor`
+    times as long as the `context` positions of training.
+      scaling None      as they are
+              "linear"  all divided by factor
+              "base"    theta * factor^(rot/(rot-2)): the slowest pair is divided by factor, the fastest not at all
+              "bands"   a pair that makes fewer than `low` turns in `context` is divided by factor, one that makes more than `high`
+                        stays, those between are blended by their turns"""
+    if rot <= 0 or rot % 2 or theta <= 0 or factor <= 0:
+        raise ValueError("rot must be even and positive, theta and factor positive")
+    if scaling not in (None, "linear", "base", "bands"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if scaling == "bands" and not (context > 0 and high > low):
+        raise ValueError("bands need a context and low < high")
+    if scaling == "base" and rot > 2:
+        theta = theta * factor ** (rot / (rot - 2))
+    freqs = torch.tensor([theta ** (-2.0 * i / rot) for i in range(rot // 2)], dtype=torch.float64)
+    if scaling == "linear":
+        freqs = freqs / factor
+    elif scaling == "bands":
+        keep = ((context * freqs / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        freqs = keep * freqs + (1 - keep) * freqs / factor
+    return freqs.to(device)
+
+
+def tree_masks(parents):
+    """The masks of tree_decode_attention from the parents of drafted tokens: parents [S,T] (integers; a token's parent comes
+    before it, a negative number is the end of the context, T or more a token that is not there) -> int64 [S,T] on its device,
+    bit j of [s,t] set for t itself and its ancestors; 0 for a token that is not there."""
+    if parents.dim() != 2 or not 0 < parents.shape[1] <= 64:
+        raise ValueError("parents must be [S,T] with up to 64 tokens")
+    up = parents.to("cpu", torch.int64)
+    S, T = up.shape
+    if bool(((up >= torch.arange(T)) & (up < T)).any()):
+        raise ValueError("a token's parent must come before it")
+    masks = torch.zeros(S, T, dtype=torch.int64)
+    for t in range(T):
+        own = torch.full((S,), 1 << t if t < 63 else -(1 << 63), dtype=torch.int64)
+        above = masks.gather(1, up[:, t:t + 1].clamp(0, T - 1))[:, 0]
+        masks[:, t] = torch.where(up[:, t] >= T, 0, torch.where(up[:, t] >= 0, above | own, own))
+    return masks.to(parents.device)
+
+
 def _built_on_first_use(name):
     def call(*args, **kwargs):
         return getattr(native(), name)(*args, **kwargs)
@@ -441,4 +490,5 @@ try:
 except ImportError:     # not built yet: the first call builds it, or says why it cannot be loaded
     globals().update({_n: _built_on_first_use(_n) for _n in NATIVE})
 else:
-    globals().update({_n: getattr(_native, _n) for _n in NATIVE})
+    # a module built from older sources may lack some: it must not keep the package from being imported and built
+    globals().update({_n: getattr(_native, _n, None) or _built_on_first_use(_n) for _n in NATIVE})

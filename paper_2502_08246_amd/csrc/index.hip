@@ -1277,3 +1277,144 @@ extern "C" int32_t saap_recompact_index(const int32_t* off, const int32_t* len, 
                        overflow_flag);
   return launch_status();
 }
+
+// ---- append_accepted: the kept tokens of a tree ------------------------------------------------------------------------------------
+// A workgroup per (sequence, KV head).  The first wave has a lane per accepted token and does in one go what pushing them one
+// after the other would do: a token's target is its own bucket, or, in a window, the bucket of the key whose ring slot it takes;
+// of several with one target each takes the slot behind the one before it, and those that find no room are refused (they are the
+// last ones).  Ring slots of up to n_recent consecutive positions are distinct, so no token meets what another one stored.
+// Bound by latency: path -> ids -> lengths and offsets -> rows.
+constexpr int kMaxPath = 64;
+template <typename C, typename T>
+__global__ void __launch_bounds__(256)
+append_accepted_kernel(const int32_t* __restrict__ ids, const T* __restrict__ kt, const T* __restrict__ vt, const int32_t* __restrict__ path,
+                       const int32_t* __restrict__ pos_new, const int32_t* __restrict__ off, int32_t* __restrict__ len,
+                       int32_t* __restrict__ idx, C* __restrict__ Ks, C* __restrict__ Vs, const float* __restrict__ kscale,
+                       const float* __restrict__ vscale, int32_t* __restrict__ res_ids, int32_t* __restrict__ overflow, int Hkv, int Tn, int P,
+                       int Ncap, int B, int n_sink, int n_recent) {
+  __shared__ int s_node[kMaxPath], s_slot[kMaxPath], s_dst[kMaxPath], s_count;
+  const int unit = blockIdx.x, s = unit / Hkv, tid = threadIdx.x;
+  const int W = n_sink + n_recent, runs = res_ids ? B + 1 : B;
+  if (tid < kMaxPath) {
+    const int i = tid, node = i < P ? path[(size_t)s * P + i] : -1;
+    const unsigned long long there = __ballot((unsigned)node < (unsigned)Tn);
+    const int count = ~there == 0ull ? 64 : __ffsll(~there) - 1;
+    const int32_t* o = off + (size_t)unit * (runs + 1);
+    int32_t* l = len + (size_t)unit * runs;
+    int32_t* ix = idx + (size_t)unit * Ncap;
+    int32_t* rid = res_ids + (size_t)unit * W;
+    const bool live = i < count;
+    const int id = live ? ids[(size_t)unit * Tn + node] : -1;
+    const int first = live && pos_new ? pos_new[s] : 0, pos = !pos_new ? 0x7fffffff : first < 0 || first > 0x7fffffff - i ? -1 : first + i;
+    // -1: refused   0: slot of a window that is still filling   1: ring slot, a key is displaced   2: straight into its bucket
+    const int kind = !live || (unsigned)id >= (unsigned)B ? -1 : !res_ids ? 2 : pos < 0 ? -1 : pos < W ? 0 : n_recent > 0 ? 1 : 2;
+    const int res_base = res_ids ? o[B] : 0;
+    int slot = -1, dst = -1, target = -1, moved = -1, ring = -1;
+    if (kind == 0) {
+      ring = pos;
+      slot = res_base + pos;
+    } else if (kind == 1) {
+      ring = n_sink + (pos - n_sink) % n_recent;
+      target = rid[ring];
+      moved = ix[res_base + ring];
+      if ((unsigned)target >= (unsigned)B) target = -1;  // pushes out of order, foreign state: refused
+    } else if (kind == 2) {
+      target = id;
+    }
+    int rank = 0, same = 0;
+    for (int j = 0; j < count; ++j) {
+      const bool eq = __builtin_amdgcn_readlane(target, j) == target;
+      same += eq;
+      rank += eq && j < i;
+    }
+    const int cur = target >= 0 ? l[target] : 0, at = target >= 0 ? o[target] : 0, room = target >= 0 ? o[target + 1] - at - cur : 0;
+    if (target >= 0 && rank < room) {
+      dst = at + cur + rank;
+      slot = kind == 1 ? res_base + ring : dst;
+      if (rank == min(same, room) - 1) l[target] = cur + rank + 1;
+    }
+    const unsigned long long filled = __ballot(kind == 0);
+    if (i == 0 && filled) l[B] += __popcll(filled);
+    if (slot >= 0) {
+      if (kind == 1) ix[dst] = moved;
+      if (ring >= 0) rid[ring] = id;
+      ix[slot] = pos_new ? pos : -2;
+    } else if (live) {
+      *overflow = 1;
+    }
+    s_node[i] = node;
+    s_slot[i] = slot;
+    s_dst[i] = kind == 1 ? dst : -1;
+    if (i == 0) s_count = count;
+  }
+  __syncthreads();
+  // 16 lanes to a row, K and V, eight tokens at a time: the displaced row into its bucket, the new one into its slot
+  const bool is_v = (tid >> 4) & 1;
+  const int piece = (tid & 15) * 8;
+  C* cache = (is_v ? Vs : Ks) + (size_t)unit * Ncap * kD + piece;
+  const T* rows = (is_v ? vt : kt) + (size_t)unit * Tn * kD + piece;
+  const float* scale = is_v ? vscale : kscale;
+  const float inv = scale ? 1.0f / scale[unit] : 1.f;
+  for (int i = tid >> 5; i < s_count; i += 8) {
+    const int slot = s_slot[i], dst = s_dst[i];
+    if (slot < 0) continue;
+    struct alignas(sizeof(C) * 8 < 16 ? sizeof(C) * 8 : 16) Piece { C v[8]; };
+    struct alignas(16) Given { T v[8]; };
+    const Given x = *reinterpret_cast<const Given*>(rows + (size_t)s_node[i] * kD);
+    Piece* to = reinterpret_cast<Piece*>(cache + (size_t)slot * kD);
+    if (dst >= 0) *reinterpret_cast<Piece*>(cache + (size_t)dst * kD) = *to;
+    Piece y;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y.v[j] = to_cache<C, T>(x.v[j], inv);
+    *to = y;
+  }
+}
+
+static int32_t append_accepted(const int32_t* ids, const void* kt, const void* vt, const int32_t* path, const int32_t* pos_new,
+                               const int32_t* off, int32_t* len, int32_t* idx, void* Ks, void* Vs, const float* kscale, const float* vscale,
+                               int32_t* res_ids, int32_t* overflow, int32_t S, int32_t Hkv, int32_t T, int32_t P, int32_t Ncap, int32_t B,
+                               int32_t d, int32_t dtype, bool fp8, int32_t n_sink, int32_t n_recent, void* stream) {
+  if (!ids || !kt || !vt || !path || !off || !len || !idx || !Ks || !Vs || !overflow || (fp8 && (!kscale || !vscale))) return SAAP_INVALID_ARG;
+  for (const void* t : {kt, vt, (const void*)Ks, (const void*)Vs})
+    if (!aligned16(t)) return SAAP_INVALID_ARG;
+  if (S <= 0 || Hkv <= 0 || T <= 0 || P <= 0 || Ncap <= 0 || B <= 0 || n_sink < 0 || n_recent < 0) return SAAP_INVALID_ARG;
+  if (dtype != SAAP_F32 && dtype != SAAP_BF16) return SAAP_INVALID_ARG;
+  if (res_ids ? !pos_new || (long long)n_sink + n_recent > Ncap : n_sink || n_recent) return SAAP_INVALID_ARG;
+  if (d != kD || B > SAAP_MAX_BUCKETS || P > kMaxPath || (n_recent > 0 && P > n_recent)) return SAAP_UNSUPPORTED;
+  const long long units = (long long)S * Hkv;
+  if (units > 0x7fffffLL) return SAAP_UNSUPPORTED;
+  hipStream_t hs = static_cast<hipStream_t>(stream);
+  auto launch = [&](auto kernel, auto* k, auto* v, auto* K, auto* V) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)units), dim3(256), 0, hs, ids, k, v, path, pos_new, off, len, idx, K, V, kscale, vscale, res_ids,
+                       overflow, Hkv, T, P, Ncap, B, n_sink, n_recent);
+  };
+  if (fp8)
+    launch(append_accepted_kernel<fp8_t, bf16_t>, static_cast<const bf16_t*>(kt), static_cast<const bf16_t*>(vt), static_cast<fp8_t*>(Ks),
+           static_cast<fp8_t*>(Vs));
+  else if (dtype == SAAP_BF16)
+    launch(append_accepted_kernel<bf16_t, bf16_t>, static_cast<const bf16_t*>(kt), static_cast<const bf16_t*>(vt), static_cast<bf16_t*>(Ks),
+           static_cast<bf16_t*>(Vs));
+  else
+    launch(append_accepted_kernel<float, float>, static_cast<const float*>(kt), static_cast<const float*>(vt), static_cast<float*>(Ks),
+           static_cast<float*>(Vs));
+  return launch_status();
+}
+
+extern "C" int32_t saap_append_accepted(const int32_t* bucket_ids, const void* k_tree, const void* v_tree, const int32_t* path,
+                                        const int32_t* pos_new, const int32_t* off, int32_t* len, int32_t* idx, void* Ksorted, void* Vsorted,
+                                        int32_t* resident_ids, int32_t* overflow_flag, int32_t S, int32_t Hkv, int32_t T, int32_t P,
+                                        int32_t Ncap, int32_t B, int32_t d, int32_t dtype, int32_t n_sink, int32_t n_recent, void* stream) {
+  const Call call(stream);
+  return append_accepted(bucket_ids, k_tree, v_tree, path, pos_new, off, len, idx, Ksorted, Vsorted, nullptr, nullptr, resident_ids,
+                         overflow_flag, S, Hkv, T, P, Ncap, B, d, dtype, false, n_sink, n_recent, stream);
+}
+
+extern "C" int32_t saap_append_accepted_fp8(const int32_t* bucket_ids, const void* k_tree, const void* v_tree, const int32_t* path,
+                                            const int32_t* pos_new, const int32_t* off, int32_t* len, int32_t* idx, uint8_t* K8, uint8_t* V8,
+                                            const float* kscale, const float* vscale, int32_t* resident_ids, int32_t* overflow_flag, int32_t S,
+                                            int32_t Hkv, int32_t T, int32_t P, int32_t Ncap, int32_t B, int32_t d, int32_t n_sink,
+                                            int32_t n_recent, void* stream) {
+  const Call call(stream);
+  return append_accepted(bucket_ids, k_tree, v_tree, path, pos_new, off, len, idx, K8, V8, kscale, vscale, resident_ids, overflow_flag, S, Hkv,
+                         T, P, Ncap, B, d, SAAP_BF16, true, n_sink, n_recent, stream);
+}

@@ -15,6 +15,8 @@ size_t mass_workspace_bytes(long long units, int G, int B);
 size_t mass_batch_workspace_bytes(long long units, long long R, int B);
 size_t update_from_ids_workspace_bytes(long long units, int N, int B);
 size_t train_workspace_bytes(long long Hw, long long R, int d, int hidden, int B);
+size_t rotate_grads_workspace_bytes(long long tokens, int Hq, int Hkv);
+size_t tree_workspace_bytes(long long units, int T, int G, int runs, long long lists, int dtype);
 
 int current_device() {
   int dev = -1;
@@ -161,6 +163,12 @@ extern "C" size_t saap_workspace_bytes(int32_t op, const saap_shape* sh) {
     case SAAP_OP_BUCKET_ATTENTION_MASS:
       if (S <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || sh->B <= 0) return 0;
       return mass_workspace_bytes(S * Hkv, (int)(Hq / Hkv), sh->B);
+    case SAAP_OP_NORM_ROTATE_GRADS:
+      if (S <= 0 || Hq < 0 || Hkv < 0 || Hq + Hkv <= 0 || Hq > 4096 || Hkv > 4096 || sh->N <= 0) return 0;
+      return rotate_grads_workspace_bytes(S * sh->N, (int)Hq, (int)Hkv);
+    case SAAP_OP_TREE_DECODE_ATTENTION:
+      if (S <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || sh->N <= 0 || sh->B < 0 || sh->nprobe < 0) return 0;
+      return tree_workspace_bytes(S * Hkv, sh->N, (int)(Hq / Hkv), sh->B, (sh->mode ? (long long)sh->N : 1LL) * sh->nprobe, sh->dtype);
     default:
       return 0;
   }

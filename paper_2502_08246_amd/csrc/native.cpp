@@ -14,6 +14,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <ATen/ops/zeros.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/Dtype.h>
@@ -972,6 +973,337 @@ SAAP_FUNCTION(adam_update) {
   SAAP_END
 }
 
+// ---- drafted tokens ------------------------------------------------------------------------------------
+// What these calls read is looked at before it is passed on: type, shape, and that it is on the current device, whose stream
+// the kernels are put on.
+void want(const Tensor& t, at::ScalarType type, at::IntArrayRef shape, const char* name) {
+  if (t.scalar_type() != type) {
+    PyErr_Format(PyExc_TypeError, "%s must be %s, not %s", name, c10::toString(type), c10::toString(t.scalar_type()));
+    throw python_error();
+  }
+  if (t.sizes() != shape) {
+    PyErr_Format(PyExc_ValueError, "%s has the wrong shape", name);
+    throw python_error();
+  }
+}
+void want_here(const Tensor& t) {
+  if (!t.is_cuda()) raise_value("SAAP tensors must live in GPU memory; there is no CPU path");
+  if (t.device().index() != c10::hip::current_device()) raise_value("SAAP tensors must be on the current device");
+}
+template <typename T> T* given(const Args& a, int i, at::ScalarType type, at::IntArrayRef shape, const char* name) {
+  if (!a.has(i)) return nullptr;
+  want(a.tensor(i), type, shape, name);
+  want_here(a.tensor(i));
+  return ptr_as<T>(a.tensor(i));
+}
+// A tensor that the call needs, with want()'s checks.
+template <typename T> T* needed(const Args& a, int i, at::ScalarType type, at::IntArrayRef shape, const char* name) {
+  want(a.tensor(i), type, shape, name);
+  want_here(a.tensor(i));
+  return ptr_as<T>(a.tensor(i));
+}
+PyObject* tuple_or_none(std::initializer_list<const Out*> outs) {        // nullptr: None
+  PyObject* r = PyTuple_New((Py_ssize_t)outs.size());
+  if (!r) throw python_error();
+  Py_ssize_t i = 0;
+  for (const Out* o : outs) {
+    PyObject* x = Py_None;
+    if (o) x = o->object();
+    else Py_INCREF(x);
+    if (!x) {
+      Py_DECREF(r);
+      throw python_error();
+    }
+    PyTuple_SET_ITEM(r, i++, x);
+  }
+  return r;
+}
+
+// q or k [S,T,H,d] as norm_rotate takes it: heads and features dense, tokens any distance apart, sequences T tokens.
+int64_t token_stride(const Tensor& t) {
+  want_dims(t, 4);
+  const int64_t S = t.size(0), T = t.size(1), H = t.size(2), d = t.size(3);
+  const int64_t stride = T > 1 ? t.stride(1) : S > 1 ? t.stride(0) : H * d;
+  if ((d > 1 && t.stride(3) != 1) || (H > 1 && t.stride(2) != d) || (S > 1 && T > 1 && t.stride(0) != T * stride) || stride < H * d)
+    raise_value("q and k must have dense heads and equally spaced tokens");
+  return stride;
+}
+struct Rotation {
+  saap_rotation r{};
+  const Tensor *q, *k, *any;
+  void *pq = nullptr, *pk = nullptr;
+  // positions of the arguments: q, k, positions, freqs at 0..3; q_weight, k_weight, norm, eps, pairs, magnitude from i on
+  Rotation(const Args& a, int i) : q(a.maybe(0)), k(a.maybe(1)), any(q ? q : k) {
+    if (!any) raise_value("q or k must be given");
+    for (const Tensor* t : {q, k})
+      if (t) {
+        want_dims(*t, 4);
+        want_here(*t);
+        if (t->size(0) != any->size(0) || t->size(1) != any->size(1) || t->size(3) != any->size(3)) raise_value("q and k must be of the same tokens");
+        if (t->scalar_type() != any->scalar_type()) raise_type("q and k must be of one dtype");
+        (t == q ? r.q_stride : r.k_stride) = token_stride(*t);
+        (t == q ? r.Hq : r.Hkv) = size(*t, 2);
+        (t == q ? pq : pk) = t->data_ptr();
+      }
+    r.S = size(*any, 0); r.T = size(*any, 1); r.d = size(*any, 3);
+    r.dtype = dtype_code(*any);
+    r.positions = needed<int32_t>(a, 2, at::kInt, {r.S, r.T}, "positions");
+    const Tensor& f = a.tensor(3);
+    want_dims(f, 1);
+    r.freqs = needed<double>(a, 3, at::kDouble, {f.size(0)}, "freqs");
+    r.rot = 2 * size(f, 0);
+    int heads = -1;
+    for (int n = 0; n < 2; ++n) {
+      if (!a.has(i + n)) continue;
+      const Tensor& w = a.tensor(i + n);
+      const int H = n ? r.Hkv : r.Hq;
+      if (!(n ? k : q)) raise_value("a weight without its tensor");
+      if (heads >= 0 && heads != (w.dim() == 2)) raise_value("q_weight and k_weight must both be [d] or both [heads,d]");
+      heads = w.dim() == 2;
+      const float* pw = heads ? needed<float>(a, i + n, at::kFloat, {H, r.d}, "weight") : needed<float>(a, i + n, at::kFloat, {r.d}, "weight");
+      (n ? r.k_weight : r.q_weight) = pw;
+    }
+    r.weight_per_head = heads == 1;
+    r.norm = a.truth(i + 2, true);
+    r.eps = (float)a.real(i + 3, 1e-6);
+    r.pairs = a.truth(i + 4, false);
+    r.magnitude = (float)a.real(i + 5, 1.0);
+  }
+};
+
+SAAP_FUNCTION(norm_rotate) {
+  SAAP_BEGIN(4, "q", "k", "positions", "freqs", "q_weight", "k_weight", "norm", "eps", "pairs", "magnitude", "q_features", "k_features",
+             "q_rot", "q_feat", "k_rot", "k_feat")
+  const Rotation t(a, 4);
+  const saap_rotation& r = t.r;
+  const bool qf = t.q && a.truth(10, true), kf = t.k && a.truth(11, true);
+  const at::ScalarType type = t.any->scalar_type();
+  const std::vector<int64_t> qs{r.S, r.T, r.Hq, r.d}, ks{r.S, r.Hkv, r.T, r.d}, none{0};
+  void* p[4];
+  Out q_rot(a, t.q ? 12 : -1, t.q ? qs : none, type, *t.any), q_feat(a, qf ? 13 : -1, qf ? qs : none, type, *t.any);
+  Out k_rot(a, t.k ? 14 : -1, t.k ? ks : none, type, *t.any), k_feat(a, kf ? 15 : -1, kf ? ks : none, type, *t.any);
+  Out* outs[4] = {t.q ? &q_rot : nullptr, qf ? &q_feat : nullptr, t.k ? &k_rot : nullptr, kf ? &k_feat : nullptr};
+  for (int i = 0; i < 4; ++i) {
+    if (!outs[i] && a.has(12 + i)) raise_value("an output that was not asked for");
+    if (outs[i]) {
+      want(outs[i]->t, type, i < 2 ? qs : ks, "an output");
+      want_here(outs[i]->t);
+    }
+    p[i] = outs[i] ? ptr(outs[i]->t) : nullptr;
+  }
+  void* st = stream();
+  call("saap_norm_rotate", [&] { return saap_norm_rotate(&r, t.pq, t.pk, p[1], p[0], p[3], p[2], st); });
+  return tuple_or_none({outs[0], outs[1], outs[2], outs[3]});
+  SAAP_END
+}
+
+SAAP_FUNCTION(norm_rotate_grads) {
+  SAAP_BEGIN(8, "q", "k", "positions", "freqs", "g_q_rot", "g_q_feat", "g_k_rot", "g_k_feat", "q_weight", "k_weight", "norm", "eps", "pairs",
+             "magnitude", "ws")
+  const Rotation t(a, 8);
+  const saap_rotation& r = t.r;
+  const at::ScalarType type = t.any->scalar_type();
+  const std::vector<int64_t> qs{r.S, r.T, r.Hq, r.d}, ks{r.S, r.Hkv, r.T, r.d}, none{0};
+  const void* g[4];
+  for (int i = 0; i < 4; ++i) {
+    if (a.has(4 + i) && !(i < 2 ? t.q : t.k)) raise_value("a gradient without its tensor");
+    g[i] = given<void>(a, 4 + i, type, i < 2 ? qs : ks, "a gradient");
+  }
+  const std::vector<int64_t> dks{r.S, r.T, r.Hkv, r.d};
+  Out dq(a, -1, t.q ? qs : none, type, *t.any), dk(a, -1, t.k ? dks : none, type, *t.any);
+  Out dqw(a, -1, r.q_weight ? a.tensor(8).sizes() : at::IntArrayRef(none), at::kFloat, *t.any);
+  Out dkw(a, -1, r.k_weight ? a.tensor(9).sizes() : at::IntArrayRef(none), at::kFloat, *t.any);
+  saap_shape sh = shape_of(r.S, r.Hq, r.Hkv);
+  sh.N = r.T;
+  const Ws ws(a, 14, *t.any, SAAP_OP_NORM_ROTATE_GRADS, sh);
+  void *pdq = t.q ? ptr(dq.t) : nullptr, *pdk = t.k ? ptr(dk.t) : nullptr;
+  float *pqw = r.q_weight ? ptr_as<float>(dqw.t) : nullptr, *pkw = r.k_weight ? ptr_as<float>(dkw.t) : nullptr;
+  void* st = stream();
+  call("saap_norm_rotate_grads", [&] {
+    return saap_norm_rotate_grads(&r, t.pq, t.pk, g[1], g[0], g[3], g[2], pdq, pdk, pqw, pkw, ws.p, ws.bytes, st);
+  });
+  return tuple_or_none({t.q ? &dq : nullptr, t.k ? &dk : nullptr, r.q_weight ? &dqw : nullptr, r.k_weight ? &dkw : nullptr});
+  SAAP_END
+}
+
+// The arguments that the four tree calls share.  q, K, V and, for an 8-bit cache, kscale, vscale come first; from `i` on k_tree,
+// v_tree, tree; from `o` on softcap, slopes, pos, starts, out_dtype, out, lse.
+struct TreeArgs {
+  saap_tree t{};
+  int32_t rows, dtype;
+  void *q, *K, *V;
+  const float *kscale = nullptr, *vscale = nullptr;
+  const Tensor* qt;
+  TreeArgs(const Args& a, bool fp8, int i, int o) {
+    const Tensor &qq = a.tensor(0), &k = a.tensor(1);
+    qt = &qq;
+    want_dims(qq, 4);
+    want_dims(k, 4);
+    t.S = size(qq, 0); t.T = size(qq, 1); t.Hq = size(qq, 2); t.d = size(qq, 3); t.Hkv = size(k, 1); rows = size(k, 2);
+    const at::ScalarType type = qq.scalar_type(), cache = fp8 ? at::kByte : type;
+    if (fp8 && type != at::kBFloat16) raise_type("q must be bf16, K8 and V8 uint8");
+    dtype = dtype_code(qq);
+    want_here(qq);
+    q = ptr(qq);
+    K = needed<void>(a, 1, cache, {t.S, t.Hkv, rows, t.d}, "the cache");
+    V = needed<void>(a, 2, cache, {t.S, t.Hkv, rows, t.d}, "the cache");
+    if (fp8) {
+      kscale = needed<float>(a, 3, at::kFloat, {t.S, t.Hkv}, "kscale");
+      vscale = needed<float>(a, 4, at::kFloat, {t.S, t.Hkv}, "vscale");
+    }
+    t.k_tree = given<void>(a, i, type, {t.S, t.Hkv, t.T, t.d}, "k_tree");
+    t.v_tree = given<void>(a, i + 1, type, {t.S, t.Hkv, t.T, t.d}, "v_tree");
+    t.tree = given<int64_t>(a, i + 2, at::kLong, {t.S, t.T}, "tree");
+    t.softcap = (float)a.real(o, 0.0);
+    t.slopes = given<float>(a, o + 1, at::kFloat, {t.Hq}, "slopes");
+    t.pos = given<int32_t>(a, o + 2, at::kInt, {t.S, t.T}, "pos");
+    t.starts = given<int32_t>(a, o + 3, at::kInt, {t.S, t.T}, "starts");
+  }
+};
+struct TreeOut {
+  Out out, lse;
+  void* p;
+  float* pl;
+  int32_t code;
+  TreeOut(const Args& a, const TreeArgs& t, int o)
+      : out(a, o + 5, {t.t.S, t.t.T, t.t.Hq, t.t.d}, a.dtype(o + 4, at::kFloat), *t.qt), lse(a, o + 6, {t.t.S, t.t.T, t.t.Hq}, at::kFloat, *t.qt) {
+    code = dtype_code(out.t);
+    want(out.t, out.t.scalar_type(), {t.t.S, t.t.T, t.t.Hq, t.t.d}, "out");
+    want(lse.t, at::kFloat, {t.t.S, t.t.T, t.t.Hq}, "lse");
+    want_here(out.t);
+    want_here(lse.t);
+    p = ptr(out.t);
+    pl = ptr_as<float>(lse.t);
+  }
+};
+saap_shape tree_shape(const TreeArgs& t, int runs, int nprobe, int per_token) {
+  saap_shape sh = shape_of(t.t.S, t.t.Hq, t.t.Hkv, per_token);
+  sh.N = t.t.T; sh.B = runs; sh.nprobe = nprobe; sh.dtype = t.dtype;
+  return sh;
+}
+
+PyObject* tree_lists(const Args& a, bool fp8, const char* name) {
+  const int n = fp8 ? 5 : 3;                             // off, ln, selected, scale, k_tree, v_tree, tree, idx, resident_run, ...
+  TreeArgs t(a, fp8, n + 4, n + 9);
+  const Tensor &ln = a.tensor(n + 1), &sel = a.tensor(n + 2);
+  want_dims(ln, 3);
+  const int32_t runs = size(ln, 2), per_token = sel.dim() == 4;
+  if (sel.dim() != 3 && sel.dim() != 4) raise_value("selected must be [S,Hkv,nprobe] or [S,T,Hkv,nprobe]");
+  const int32_t nprobe = size(sel, per_token ? 3 : 2);
+  const int32_t* off = needed<int32_t>(a, n, at::kInt, {t.t.S, t.t.Hkv, (int64_t)runs + 1}, "off");
+  const int32_t* len = needed<int32_t>(a, n + 1, at::kInt, {t.t.S, t.t.Hkv, runs}, "ln");
+  const int32_t* lists = per_token ? needed<int32_t>(a, n + 2, at::kInt, {t.t.S, t.t.T, t.t.Hkv, nprobe}, "selected")
+                                   : needed<int32_t>(a, n + 2, at::kInt, {t.t.S, t.t.Hkv, nprobe}, "selected");
+  if (nprobe == 0) lists = nullptr;
+  t.t.scale = (float)a.real(n + 3);
+  t.t.idx = given<int32_t>(a, n + 7, at::kInt, {t.t.S, t.t.Hkv, t.rows}, "idx");
+  const int32_t resident = a.integer(n + 8, -1);
+  const TreeOut o(a, t, n + 9);
+  const Ws ws(a, n + 16, *t.qt, SAAP_OP_TREE_DECODE_ATTENTION, tree_shape(t, runs, nprobe, per_token));
+  void* st = stream();
+  call(name, [&] {
+    return fp8 ? saap_tree_decode_attention_fp8(&t.t, t.q, static_cast<uint8_t*>(t.K), static_cast<uint8_t*>(t.V), t.kscale, t.vscale, off,
+                                                len, lists, nprobe, per_token, resident, o.p, o.code, o.pl, t.rows, runs, ws.p, ws.bytes, st)
+               : saap_tree_decode_attention(&t.t, t.q, t.K, t.V, off, len, lists, nprobe, per_token, resident, o.p, o.code, o.pl, t.rows, runs,
+                                            t.dtype, ws.p, ws.bytes, st);
+  });
+  return tuple_of({&o.out, &o.lse});
+}
+PyObject* tree_dense(const Args& a, bool fp8, const char* name) {
+  const int n = fp8 ? 5 : 3;                             // scale, k_tree, v_tree, tree, n_keys, ...
+  TreeArgs t(a, fp8, n + 1, n + 5);
+  t.t.scale = (float)a.real(n);
+  const int32_t* n_keys = given<int32_t>(a, n + 4, at::kInt, {t.t.S}, "n_keys");
+  const TreeOut o(a, t, n + 5);
+  const Ws ws(a, n + 12, *t.qt, SAAP_OP_TREE_DECODE_ATTENTION, tree_shape(t, 0, 0, 0));
+  void* st = stream();
+  call(name, [&] {
+    return fp8 ? saap_dense_tree_decode_attention_fp8(&t.t, t.q, static_cast<uint8_t*>(t.K), static_cast<uint8_t*>(t.V), t.kscale, t.vscale,
+                                                      n_keys, o.p, o.code, o.pl, t.rows, ws.p, ws.bytes, st)
+               : saap_dense_tree_decode_attention(&t.t, t.q, t.K, t.V, n_keys, o.p, o.code, o.pl, t.rows, t.dtype, ws.p, ws.bytes, st);
+  });
+  return tuple_of({&o.out, &o.lse});
+}
+
+SAAP_FUNCTION(tree_decode_attention) {
+  SAAP_BEGIN(7, "q", "Ks", "Vs", "off", "ln", "selected", "scale", "k_tree", "v_tree", "tree", "idx", "resident_run", "softcap", "slopes", "pos",
+             "starts", "out_dtype", "out", "lse", "ws")
+  return tree_lists(a, false, "saap_tree_decode_attention");
+  SAAP_END
+}
+SAAP_FUNCTION(tree_decode_attention_fp8) {
+  SAAP_BEGIN(9, "q", "K8", "V8", "kscale", "vscale", "off", "ln", "selected", "scale", "k_tree", "v_tree", "tree", "idx", "resident_run",
+             "softcap", "slopes", "pos", "starts", "out_dtype", "out", "lse", "ws")
+  return tree_lists(a, true, "saap_tree_decode_attention_fp8");
+  SAAP_END
+}
+SAAP_FUNCTION(dense_tree_decode_attention) {
+  SAAP_BEGIN(4, "q", "K", "V", "scale", "k_tree", "v_tree", "tree", "n_keys", "softcap", "slopes", "pos", "starts", "out_dtype", "out", "lse",
+             "ws")
+  return tree_dense(a, false, "saap_dense_tree_decode_attention");
+  SAAP_END
+}
+SAAP_FUNCTION(dense_tree_decode_attention_fp8) {
+  SAAP_BEGIN(6, "q", "K8", "V8", "kscale", "vscale", "scale", "k_tree", "v_tree", "tree", "n_keys", "softcap", "slopes", "pos", "starts",
+             "out_dtype", "out", "lse", "ws")
+  return tree_dense(a, true, "saap_dense_tree_decode_attention_fp8");
+  SAAP_END
+}
+
+PyObject* accept(const Args& a, bool fp8, const char* name) {
+  const Tensor &ids = a.tensor(0), &kt = a.tensor(1), &path = a.tensor(3), &ln = a.tensor(6), &idx = a.tensor(7);
+  want_dims(ids, 3);
+  want_dims(kt, 4);
+  want_dims(path, 2);
+  want_dims(ln, 3);
+  want_dims(idx, 3);
+  const int n = fp8 ? 12 : 10;                           // resident_ids, n_sink, n_recent, overflow_flag
+  const int32_t S = size(ids, 0), Hkv = size(ids, 1), T = size(ids, 2), d = size(kt, 3), P = size(path, 1), Ncap = size(idx, 2);
+  const int32_t n_sink = a.integer(n + 1, 0), n_recent = a.integer(n + 2, 0), B = size(ln, 2) - (a.has(n) ? 1 : 0);
+  const at::ScalarType type = kt.scalar_type(), cache = fp8 ? at::kByte : type;
+  if (fp8 && type != at::kBFloat16) raise_type("bf16 rows expected");
+  const int32_t dt = dtype_code(kt);
+  const int32_t* pi = needed<int32_t>(a, 0, at::kInt, {S, Hkv, T}, "bucket_ids");
+  const void* pk = needed<void>(a, 1, type, {S, Hkv, T, d}, "k_tree");
+  const void* pv = needed<void>(a, 2, type, {S, Hkv, T, d}, "v_tree");
+  const int32_t* pp = needed<int32_t>(a, 3, at::kInt, {S, P}, "path");
+  const int32_t* pos = given<int32_t>(a, 4, at::kInt, {S}, "pos_new");
+  const int32_t* off = needed<int32_t>(a, 5, at::kInt, {S, Hkv, (int64_t)size(ln, 2) + 1}, "off");
+  int32_t* len = needed<int32_t>(a, 6, at::kInt, {S, Hkv, size(ln, 2)}, "ln");
+  int32_t* ix = needed<int32_t>(a, 7, at::kInt, {S, Hkv, Ncap}, "idx");
+  void* K = needed<void>(a, 8, cache, {S, Hkv, Ncap, d}, "the cache");
+  void* V = needed<void>(a, 9, cache, {S, Hkv, Ncap, d}, "the cache");
+  const float* ks = fp8 ? needed<float>(a, 10, at::kFloat, {S, Hkv}, "kscale") : nullptr;
+  const float* vs = fp8 ? needed<float>(a, 11, at::kFloat, {S, Hkv}, "vscale") : nullptr;
+  int32_t* res = given<int32_t>(a, n, at::kInt, {S, Hkv, (int64_t)n_sink + n_recent}, "resident_ids");
+  Out flag = flag_buffer(a, n + 3, kt);
+  if (flag.t.scalar_type() != at::kInt || flag.t.numel() < 1) raise_type("overflow_flag must be int32");
+  want_here(flag.t);
+  int32_t* pf = ptr_as<int32_t>(flag.t);
+  // a window of no slots is an empty tensor without an address
+  int32_t nothing = 0;
+  if (a.has(n) && !res) res = &nothing;
+  void* st = stream();
+  call(name, [&] {
+    return fp8 ? saap_append_accepted_fp8(pi, pk, pv, pp, pos, off, len, ix, static_cast<uint8_t*>(K), static_cast<uint8_t*>(V), ks, vs, res, pf, S,
+                                          Hkv, T, P, Ncap, B, d, n_sink, n_recent, st)
+               : saap_append_accepted(pi, pk, pv, pp, pos, off, len, ix, K, V, res, pf, S, Hkv, T, P, Ncap, B, d, dt, n_sink, n_recent, st);
+  });
+  return flag.object();
+}
+SAAP_FUNCTION(append_accepted) {
+  SAAP_BEGIN(10, "bucket_ids", "k_tree", "v_tree", "path", "pos_new", "off", "ln", "idx", "Ks", "Vs", "resident_ids", "n_sink", "n_recent",
+             "overflow_flag")
+  return accept(a, false, "saap_append_accepted");
+  SAAP_END
+}
+SAAP_FUNCTION(append_accepted_fp8) {
+  SAAP_BEGIN(12, "bucket_ids", "k_tree", "v_tree", "path", "pos_new", "off", "ln", "idx", "K8", "V8", "kscale", "vscale", "resident_ids",
+             "n_sink", "n_recent", "overflow_flag")
+  return accept(a, true, "saap_append_accepted_fp8");
+  SAAP_END
+}
+
 // ---- module ------------------------------------------------------------------------------------------
 SAAP_FUNCTION(workspace) {
   SAAP_BEGIN(2, "nbytes", "device_index", "asked_for")
@@ -1067,6 +1399,48 @@ PyMethodDef methods[] = {
                 "out_dtype=None, out=None, lse=None, ws=None)\n--\n\n"
                 "q [S,Tq,Hq,d]; position-ordered K,V [S,Hkv,Nt,d]; Ks,Vs,off,ln,idx from build_bucket_index over them;\n"
                 "selected int32 [S,Hkv,Tq,nprobe]; pos0 int32 [S] -> out [S,Tq,Hq,d], lse fp32 [S,Tq,Hq]."),
+    SAAP_METHOD(norm_rotate,
+                "norm_rotate(q, k, positions, freqs, q_weight=None, k_weight=None, norm=True, eps=1e-06, pairs=False, "
+                "magnitude=1.0, q_features=True, k_features=True, q_rot=None, q_feat=None, k_rot=None, k_feat=None)\n--\n\n"
+                "q [S,T,Hq,d], k [S,T,Hkv,d] (slices of one projection will do; either may be None), positions int32 [S,T], freqs\n"
+                "float64 [rot/2] (rotary_frequencies) -> q_rot, q_feat [S,T,Hq,d], k_rot, k_feat [S,Hkv,T,d]: the heads' norm with fp32\n"
+                "weights [d] or [heads,d], before (feat) and after (rot) the rotation of the first rot features; None where there is none."),
+    SAAP_METHOD(norm_rotate_grads,
+                "norm_rotate_grads(q, k, positions, freqs, g_q_rot, g_q_feat, g_k_rot, g_k_feat, q_weight=None, k_weight=None, "
+                "norm=True, eps=1e-06, pairs=False, magnitude=1.0, ws=None)\n--\n\n"
+                "Gradients of norm_rotate from those of its outputs (shaped as they are, or None)\n"
+                "-> dq [S,T,Hq,d], dk [S,T,Hkv,d], dq_weight, dk_weight fp32 shaped as the weights; None where there is none."),
+    SAAP_METHOD(tree_decode_attention,
+                "tree_decode_attention(q, Ks, Vs, off, ln, selected, scale, k_tree=None, v_tree=None, tree=None, idx=None, "
+                "resident_run=-1, softcap=0.0, slopes=None, pos=None, starts=None, out_dtype=None, out=None, lse=None, ws=None)"
+                "\n--\n\n"
+                "T tokens of every sequence at once: q [S,T,Hq,d]; selected [S,Hkv,nprobe] or a list per token [S,T,Hkv,nprobe];\n"
+                "k_tree, v_tree [S,Hkv,T,d] and tree int64 [S,T]: the drafted keys that a token attends, as bits (tree_masks).\n"
+                "softcap, slopes [Hq] (with pos int32 [S,T]) and starts int32 [S,T] shape and cut the scores; the last two need idx.\n"
+                "-> out [S,T,Hq,d] of out_dtype (None: float32), lse fp32 [S,T,Hq]."),
+    SAAP_METHOD(tree_decode_attention_fp8,
+                "tree_decode_attention_fp8(q, K8, V8, kscale, vscale, off, ln, selected, scale, k_tree=None, v_tree=None, tree=None, "
+                "idx=None, resident_run=-1, softcap=0.0, slopes=None, pos=None, starts=None, out_dtype=None, out=None, lse=None, "
+                "ws=None)\n--\n\n"
+                "tree_decode_attention on an 8-bit cache; q, k_tree and v_tree bf16."),
+    SAAP_METHOD(dense_tree_decode_attention,
+                "dense_tree_decode_attention(q, K, V, scale, k_tree=None, v_tree=None, tree=None, n_keys=None, softcap=0.0, "
+                "slopes=None, pos=None, starts=None, out_dtype=None, out=None, lse=None, ws=None)\n--\n\n"
+                "tree_decode_attention over every key of a packed cache K, V [S,Hkv,N,d], of n_keys int32 [S] (None: N) rows each."),
+    SAAP_METHOD(dense_tree_decode_attention_fp8,
+                "dense_tree_decode_attention_fp8(q, K8, V8, kscale, vscale, scale, k_tree=None, v_tree=None, tree=None, n_keys=None, "
+                "softcap=0.0, slopes=None, pos=None, starts=None, out_dtype=None, out=None, lse=None, ws=None)\n--\n\n"
+                "dense_tree_decode_attention on an 8-bit cache."),
+    SAAP_METHOD(append_accepted,
+                "append_accepted(bucket_ids, k_tree, v_tree, path, pos_new, off, ln, idx, Ks, Vs, resident_ids=None, n_sink=0, "
+                "n_recent=0, overflow_flag=None)\n--\n\n"
+                "The drafted tokens path int32 [S,P] (ended by -1) join the index in place, in buckets bucket_ids int32 [S,Hkv,T], as\n"
+                "append_keys (resident_ids: window_push) would add them one by one; pos_new [S]: the first one's position.\n"
+                "-> overflow_flag."),
+    SAAP_METHOD(append_accepted_fp8,
+                "append_accepted_fp8(bucket_ids, k_tree, v_tree, path, pos_new, off, ln, idx, K8, V8, kscale, vscale, "
+                "resident_ids=None, n_sink=0, n_recent=0, overflow_flag=None)\n--\n\n"
+                "append_accepted on an 8-bit cache (rows bf16)."),
     SAAP_METHOD(append_keys,
                 "append_keys(x_new, k_new, v_new, pos_new, centroids, bias, off, ln, idx, Ks, Vs, overflow_flag=None, "
                 "new_ids=None, ws=None)\n--\n\n"
