@@ -26,7 +26,7 @@ struct RotateParams {
   const float *q_weight, *k_weight;
   void *q_feat, *q_rot, *k_feat, *k_rot;                 // forward: out; backward: gradients in
   void *dq, *dk;                                         // backward: out
-  float* part;                                           // backward: [chunks][quads][4][128] sums of weight gradients
+  float* part;                                           // backward: [chunks][quads][4 per head, 1 shared][128] sums of weight gradients
   long long q_stride, k_stride;                          // elements between tokens
   long long tokens;                                      // S * T
   int T, Hq, Hkv, rot, pairs, norm, per_head;
@@ -256,44 +256,57 @@ norm_rotate_grads_kernel(RotateParams p) {
   s_dw[wave][lane][0] = make_float4(dw[0], dw[1], dw[2], dw[3]);
   s_dw[wave][lane][1] = make_float4(dw[4], dw[5], dw[6], dw[7]);
   __syncthreads();
-  if (wave) return;
-  float4 a = s_dw[0][lane][0], b = s_dw[0][lane][1];
+  // weights of all heads: one row of 16 lanes; per head: the four lane groups apart
+  const int rows = p.per_head ? 4 : 1;
+  if (wave || grp >= rows) return;
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
 #pragma unroll
-  for (int i = 1; i < kWaves; ++i) {
-    const float4 u = s_dw[i][lane][0], v = s_dw[i][lane][1];
-    a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
-    b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
-  }
-  float* to = p.part + (((size_t)blockIdx.x * p.quads + quad) * 4 + grp) * kD + sub * 8;
+  for (int i = 0; i < kWaves; ++i)
+    for (int j = grp; j < 4; j += rows) {
+      const float4 u = s_dw[i][j * 16 + sub][0], v = s_dw[i][j * 16 + sub][1];
+      a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
+      b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
+    }
+  float* to = p.part + (((size_t)blockIdx.x * p.quads + quad) * rows + grp) * kD + sub * 8;
   *reinterpret_cast<float4*>(to) = a;
   *reinterpret_cast<float4*>(to + 4) = b;
 }
 
 // The weights' gradients from the workgroups' sums, in a fixed order.  A workgroup: 16 features of one weight row (blockIdx.x:
-// 8 slices of features; blockIdx.y: weight row, q's then k's), 16 threads to a feature.
-__global__ void __launch_bounds__(256)
+// eight slices of features; blockIdx.y: weight row, q's then k's), 64 threads to a feature, eight loads in flight: some thousand
+// sums of a shared weight take 5 us (16 threads and a load at a time took 166).
+constexpr int kSumThreads = 1024, kSumParts = kSumThreads / 16;
+__global__ void __launch_bounds__(kSumThreads)
 weight_grads_kernel(const float* __restrict__ part, float* __restrict__ dq_weight, float* __restrict__ dk_weight, int chunks, int quads,
                     int q_quads, int TW, int q_rows, int per_head) {
-  __shared__ float s_sum[16][17];
-  const int f = threadIdx.x & 15, part_of = threadIdx.x >> 4;
+  __shared__ float s_sum[kSumParts][17];
+  const int f = threadIdx.x & 15, mine = threadIdx.x >> 4;
   const bool is_q = (int)blockIdx.y < q_rows;
   const int row = is_q ? blockIdx.y : blockIdx.y - q_rows;
   float* to = is_q ? dq_weight : dk_weight;
-  // the weight row's quads, and within a quad its lane groups
-  const int quad0 = (is_q ? 0 : q_quads) + (per_head ? row * TW / 4 : 0), n_quads = per_head ? 1 : is_q ? q_quads : quads - q_quads;
-  const int grp0 = per_head ? row * TW % 4 : 0, n_grp = per_head ? TW : 4;
+  // the weight row's quads, and within a quad its lane groups (shared weights: one sum to a quad)
+  const int rows = per_head ? 4 : 1, quad0 = (is_q ? 0 : q_quads) + (per_head ? row * TW / 4 : 0);
+  const int n_quads = per_head ? 1 : is_q ? q_quads : quads - q_quads, grp0 = per_head ? row * TW % 4 : 0, n_grp = per_head ? TW : 1;
   const int n = chunks * n_quads * n_grp;
+  const float* from = part + blockIdx.x * 16 + f;
   float sum = 0.f;
-  for (int i = part_of; i < n; i += 16) {
-    const int g = i % n_grp, j = i / n_grp, quad = quad0 + j % n_quads, chunk = j / n_quads;
-    sum += part[(((size_t)chunk * quads + quad) * 4 + grp0 + g) * kD + blockIdx.x * 16 + f];
-  }
-  s_sum[part_of][f] = sum;
-  __syncthreads();
-  if (part_of) return;
+  for (int i0 = mine; i0 < n; i0 += 8 * kSumParts) {
+    float v[8];
 #pragma unroll
-  for (int i = 1; i < 16; ++i) sum += s_sum[i][f];
-  to[row * kD + blockIdx.x * 16 + f] = sum;
+    for (int u = 0; u < 8; ++u) {
+      const int i = min(i0 + u * kSumParts, n - 1), g = i % n_grp, j = i / n_grp, quad = quad0 + j % n_quads, chunk = j / n_quads;
+      v[u] = from[(((size_t)chunk * quads + quad) * rows + grp0 + g) * kD];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) sum += i0 + u * kSumParts < n ? v[u] : 0.f;
+  }
+  s_sum[mine][f] = sum;
+  __syncthreads();
+  for (int step = kSumParts / 2; step > 0; step >>= 1) {
+    if (mine < step) s_sum[mine][f] += s_sum[mine + step][f];
+    __syncthreads();
+  }
+  if (mine == 0) to[row * kD + blockIdx.x * 16 + f] = s_sum[0][f];
 }
 
 // Heads of a quad are of one tensor and one quad is whole: four heads to a token, or two to two tokens, or one to four.
@@ -419,7 +432,7 @@ extern "C" int32_t saap_norm_rotate_grads(const saap_rotation* a, const void* q,
   else launch_grads<float>(p, TW, chunks, hs);
   if (p.part) {
     const int q_rows = !dq_weight ? 0 : p.per_head ? Hq : 1, k_rows = !dk_weight ? 0 : p.per_head ? Hkv : 1;
-    hipLaunchKernelGGL(weight_grads_kernel, dim3(kD / 16, (unsigned)(q_rows + k_rows)), dim3(256), 0, hs, p.part, dq_weight, dk_weight,
+    hipLaunchKernelGGL(weight_grads_kernel, dim3(kD / 16, (unsigned)(q_rows + k_rows)), dim3(kSumThreads), 0, hs, p.part, dq_weight, dk_weight,
                        (int)chunks, p.quads, p.q_quads, TW, q_rows, p.per_head);
   }
   return launch_status();

@@ -440,50 +440,51 @@ __device__ __forceinline__ void walk(const TreeParams& p, const Unit& u, Op& op,
     __builtin_amdgcn_sched_barrier(0);
     if (more) op.load_k(next.drafted ? u.kt : u.K, (unsigned)next.row, half, next.drafted);   // in flight under softmax and values
     __builtin_amdgcn_sched_barrier(0);
+    // Scores times `mult` are in units of log2.  Multiplied beforehand where they are capped or biased, in the last step otherwise.
     const float scale = at.drafted ? p.scale : u.scale;
+    float mult = scale * kLog2e;
     if (p.softcap > 0.f) {
       const float to_cap = scale / p.softcap;
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = capped(s[r] * to_cap, w.cap2);
-    } else {
+      mult = 1.f;
+    } else if (p.slopes || !(mult > 0.f)) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] *= scale * kLog2e;
+      for (int r = 0; r < 16; ++r) s[r] *= mult;
+      mult = 1.f;
     }
     unsigned word = at.word;
-    int pos[16];
-    if (p.slopes || (p.starts && !at.drafted)) {
-      s_pos[col] = at.pos;
-      wave_lds_fence();
+    const bool placed = p.slopes || (p.starts && !at.drafted);
+    // f(register, position of its key) for the lane's 16 keys
+    auto for_positions = [&](auto f) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int4 v = *reinterpret_cast<const int4*>(s_pos + 8 * j + 4 * half);
-        pos[4 * j] = v.x; pos[4 * j + 1] = v.y; pos[4 * j + 2] = v.z; pos[4 * j + 3] = v.w;
+        f(4 * j, v.x);
+        f(4 * j + 1, v.y);
+        f(4 * j + 2, v.z);
+        f(4 * j + 3, v.w);
       }
-      if (p.starts && !at.drafted)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) word &= pos[r] < w.start ? ~(1u << row_of(r, half)) : ~0u;
+    };
+    if (placed) {
+      s_pos[col] = at.pos;
+      wave_lds_fence();
+      if (p.starts && !at.drafted) for_positions([&](int r, int pos) { word &= pos < w.start ? ~(1u << row_of(r, half)) : ~0u; });
     }
     if (__ballot(word != ~0u) != 0ull)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = (word >> row_of(r, half)) & 1u ? s[r] : -INFINITY;
     // Scores relative to the row's reference.  The bias of far keys is large, its difference to the reference is not: one fused
     // step takes both, so that nothing of that difference is lost.
-    float ref = w.m == kNegBig ? 0.f : w.m;
-    f32x16_t x;
-    auto relative = [&] {
-      if (p.slopes) {
+    float ref = w.m == kNegBig ? 0.f : w.m, top = -INFINITY;
+    if (p.slopes) {
+      for_positions([&](int r, int pos) { top = fmaxf(top, s[r] + fmaf(w.slope2, (float)(pos - w.at_pos), -ref)); });
+      top = fmaxf(top, other_half(top));
+    } else {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = s[r] + fmaf(w.slope2, (float)(pos[r] - w.at_pos), -ref);
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = s[r] - ref;
-      }
-    };
-    relative();
-    float top = x[0];
-#pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, x[r]);
-    top = fmaxf(top, other_half(top));
+      for (int r = 0; r < 16; ++r) top = fmaxf(top, s[r]);
+      top = fmaf(fmaxf(top, other_half(top)), mult, -ref);
+    }
     // the reference moves when a score is more than 2^8 in weight above it, and for a row's first key
     const float limit = w.m == kNegBig ? -INFINITY : 8.f;
     if (__ballot(top > limit) != 0ull) {
@@ -498,12 +499,15 @@ __device__ __forceinline__ void walk(const TreeParams& p, const Unit& u, Op& op,
 #pragma unroll
         for (int e = 0; e < 4; ++e) w.o[e][r] *= a;
       }
-      relative();
     }
+    if (p.slopes) for_positions([&](int r, int pos) { s[r] += fmaf(w.slope2, (float)(pos - w.at_pos), -ref); });
+    else
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], mult, -ref);
     float add[4];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[r] = fast_exp2(x[r]);
+      s[r] = fast_exp2(s[r]);
       add[r % 4] = r < 4 ? s[r] : add[r % 4] + s[r];
     }
     w.l += (add[0] + add[1]) + (add[2] + add[3]);
