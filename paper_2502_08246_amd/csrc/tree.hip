@@ -23,6 +23,7 @@ namespace {
 
 constexpr int kWaves = 4;             // of a workgroup
 constexpr int kPlanThreads = 1024;
+constexpr int kWaveLds = kTile * (4 * kD + 16) / 16;      // float4 of a wave: 32 keys of fp32, or its outputs
 
 // ---- 1. the union of a unit's lists ------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(kPlanThreads)
@@ -84,18 +85,17 @@ tree_plan_kernel(TreeParams p) {
 }
 
 // A workgroup's share, RW waves with rows of their own, KW of each that share out the tiles of a unit.
-template <typename C, bool LISTS, int PARTS>
+template <typename C, bool LISTS, bool SHAPED, int PARTS>
 __global__ void __launch_bounds__(64 * kWaves, sizeof(C) == 4 ? 1 : 2)
 tree_attend_kernel(TreeParams p) {
   typedef Operands<C, PARTS> Op;
-  constexpr int kOut = 16 * 64;                          // float4 of a wave's outputs
   extern __shared__ float4 s_all[];
-  float4* s_o = s_all;                                   // [wave][16][64]; the waves' stages before that
-  float2* s_ml = reinterpret_cast<float2*>(s_o + kWaves * kOut);        // [wave][32]
+  float4* s_o = s_all;                                   // [wave][kWaveLds]: the wave's stage, then its outputs
+  float2* s_ml = reinterpret_cast<float2*>(s_o + kWaves * kWaveLds);    // [wave][32]
   int* s_pos_all = reinterpret_cast<int*>(s_ml + kWaves * kTile);       // [wave][32]
   int* s_start = s_pos_all + kWaves * kTile;             // [units + 1]
   __shared__ int s_sum[kWaves];
-  static_assert(Op::kStageBytes <= kOut * (int)sizeof(float4), "a stage in the wave's part");
+  static_assert(Op::kStageBytes <= kWaveLds * (int)sizeof(float4) && kWaveLds >= 16 * 64, "a stage or its outputs in the wave's part");
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
   const Share mine = find_share(p, s_start, s_sum, kWaves);
   if (!mine.there) return;
@@ -110,15 +110,15 @@ tree_attend_kernel(TreeParams p) {
     if (seg_end <= lo) continue;                         // a unit without tiles
     const int n = seg_end - lo, t0 = lo - first + n * kp / KW, t1 = lo - first + n * (kp + 1) / KW;
     Unit u;
-    enter<C, LISTS>(p, unit, t, g, half, u, w, op);
-    char* stage = reinterpret_cast<char*>(s_o + wave * kOut);
+    enter<C, LISTS, SHAPED>(p, unit, t, g, half, u, w, op);
+    char* stage = reinterpret_cast<char*>(s_o + wave * kWaveLds);
     int* s_pos = s_pos_all + wave * kTile;
     const size_t slot = ((size_t)blockIdx.x + unit) * p.R + row0;
     for (bool careful = false;; careful = true) {
-      walk<Op, LISTS>(p, u, op, w, t0, t1, stage, s_pos, careful);
+      walk<Op, LISTS, SHAPED>(p, u, op, w, t0, t1, stage, s_pos, careful);
       if (careful || !w.has_no_numbers()) break;
     }
-    put_partial<kWaves>(p, w, slot, left, RW, wave, s_o, s_ml);
+    put_partial<kWaves, kWaveLds>(p, w, slot, left, RW, wave, s_o, s_ml);
     lo = seg_end;
   }
 }
@@ -320,18 +320,22 @@ struct Layout {
   }
 };
 
-template <typename C, bool LISTS, int PARTS>
+template <typename C, bool LISTS, bool SHAPED, int PARTS>
 bool launch_attend(const TreeParams& p, int blocks, hipStream_t hs) {
-  const size_t lds = sizeof(float4) * kWaves * 16 * 64 + sizeof(float2) * kWaves * kTile + sizeof(int) * (kWaves * kTile + p.units + 1);
-  if (!allow_lds<tree_attend_kernel<C, LISTS, PARTS>>(lds)) return false;
-  hipLaunchKernelGGL((tree_attend_kernel<C, LISTS, PARTS>), dim3((unsigned)p.shares, (unsigned)blocks), dim3(64 * kWaves), lds, hs, p);
+  const size_t lds = sizeof(float4) * kWaves * kWaveLds + sizeof(float2) * kWaves * kTile + sizeof(int) * (kWaves * kTile + p.units + 1);
+  if (!allow_lds<tree_attend_kernel<C, LISTS, SHAPED, PARTS>>(lds)) return false;
+  hipLaunchKernelGGL((tree_attend_kernel<C, LISTS, SHAPED, PARTS>), dim3((unsigned)p.shares, (unsigned)blocks), dim3(64 * kWaves), lds, hs, p);
   return true;
+}
+template <typename C, int PARTS>
+bool launch_attend(const TreeParams& p, int blocks, bool lists, hipStream_t hs) {
+  if (shaped(p)) return lists ? launch_attend<C, true, true, PARTS>(p, blocks, hs) : launch_attend<C, false, true, PARTS>(p, blocks, hs);
+  return lists ? launch_attend<C, true, false, PARTS>(p, blocks, hs) : launch_attend<C, false, false, PARTS>(p, blocks, hs);
 }
 template <typename C>
 bool launch_attend(const TreeParams& p, int blocks, bool lists, hipStream_t hs) {
-  if constexpr (sizeof(C) == 4) return lists ? launch_attend<C, true, 1>(p, blocks, hs) : launch_attend<C, false, 1>(p, blocks, hs);
-  else if (p.out_bf16) return lists ? launch_attend<C, true, 2>(p, blocks, hs) : launch_attend<C, false, 2>(p, blocks, hs);
-  else return lists ? launch_attend<C, true, 3>(p, blocks, hs) : launch_attend<C, false, 3>(p, blocks, hs);
+  if constexpr (sizeof(C) == 4) return launch_attend<C, 1>(p, blocks, lists, hs);
+  else return p.out_bf16 ? launch_attend<C, 2>(p, blocks, lists, hs) : launch_attend<C, 3>(p, blocks, lists, hs);
 }
 
 enum class CacheType { kF32, kBf16, kFp8 };

@@ -31,9 +31,11 @@ struct TreeParams {
   float scale, softcap;
 };
 
+inline bool shaped(const TreeParams& p) { return p.softcap > 0.f || p.slopes || p.starts; }
+
 namespace {
 
-__device__ __forceinline__ int row_of(int r, int half) { return 8 * (r / 4) + 4 * half + (r % 4); }
+__device__ __forceinline__ constexpr int row_of(int r, int half) { return 8 * (r / 4) + 4 * half + (r % 4); }
 __device__ __forceinline__ void wave_lds_fence() {       // LDS written and read by one wave
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
@@ -78,31 +80,28 @@ template <bool LISTS> __device__ __forceinline__ int row_of_key(const Place& at,
 
 // The operands of a wave.  A tile's rows of K pass through LDS (`stage`): they are read whole, 16 lanes to 256 bytes (read as the
 // product takes them, 32 bytes of each of 32 rows to an instruction, the lines in flight fill the first cache and the rate stays
-// at 4.4 TB/s), and laid down with their 16-byte pieces permuted by key, so that neither side has bank conflicts.
+// at 4.4 TB/s), and laid down 16 bytes further apart than they are long: 16 lanes that take the same piece of 16 rows meet
+// different banks, and every address is one per lane and a constant.
 // Cache of bf16 rows or E4M3 codes; drafted rows are bf16 in both.
 template <typename C, int PARTS>
 struct Operands {
   typedef bf16_t Query;
   static constexpr bool kCodes = sizeof(C) == 1;
-  static constexpr int kStageBytes = kTile * 2 * kD, kPieces = kCodes ? 4 : 8;
+  static constexpr int kStageBytes = kTile * (2 * kD + 16), kPieces = kCodes ? 4 : 8;
   bf16x8_t q[8];
   u32x2_t v[16];
   static constexpr __device__ __forceinline__ bool codes(bool drafted) { return kCodes && !drafted; }
   static constexpr __device__ __forceinline__ unsigned row_bytes(bool drafted) { return codes(drafted) ? kD : 2 * kD; }
-  // 16-byte pieces of 32 rows, 64 at a time: how many times 64, the key of a lane's piece and which of the row's pieces it is
+  // 16-byte pieces of 32 rows, 64 at a time: how many times 64, and where piece `slot` is among rows of `row` bytes
   static constexpr __device__ __forceinline__ int rounds(bool drafted) { return codes(drafted) ? 4 : 8; }
-  static __device__ __forceinline__ int key_of(int slot, bool drafted) { return codes(drafted) ? slot >> 3 : slot >> 4; }
-  static __device__ __forceinline__ int piece_of(int slot, bool drafted) {
-    return codes(drafted) ? (slot & 7) ^ (slot >> 4 & 7) : (slot & 15) ^ (slot >> 4 & 15);
+  static constexpr __device__ __forceinline__ unsigned stage_row(bool drafted) { return row_bytes(drafted) + 16; }
+  static constexpr __device__ __forceinline__ int key_of(int slot, bool drafted) { return codes(drafted) ? slot >> 3 : slot >> 4; }
+  static constexpr __device__ __forceinline__ unsigned piece_of(int slot, bool drafted) { return (codes(drafted) ? slot & 7 : slot & 15) * 16; }
+  // byte offset of a lane's four features of key row_of(i, 0) + 4 half, rows `row` bytes apart
+  static constexpr __device__ __forceinline__ unsigned v_offset(int i, int col, int half, bool drafted, unsigned row) {
+    return row_of(i, 0) * row + (half * 4 * row + col * v_bytes(drafted));
   }
-  // the same for 32 rows that lie together: byte offset of a lane's piece, and of its four features of key row_of(i, 0) + 4 half
-  static __device__ __forceinline__ unsigned k_offset(int i, int lane, bool drafted) {
-    if (codes(drafted)) return i * 1024 + ((lane >> 3) * kD + (((lane & 7) ^ (lane >> 4)) * 16 ^ (i & 1) * 64));
-    return i * 1024 + ((lane >> 4) * (2 * kD) + (((lane & 15) ^ (lane >> 4)) * 16 ^ (i & 3) * 64));
-  }
-  static __device__ __forceinline__ unsigned v_offset(int i, int col, int half, bool drafted) {
-    return row_of(i, 0) * row_bytes(drafted) + (codes(drafted) ? half * 4 * kD + col * 4 : half * 8 * kD + col * 8);
-  }
+  static constexpr __device__ __forceinline__ unsigned v_bytes(bool drafted) { return codes(drafted) ? 4 : 8; }
   // the features of a lane's half in step `st` of the first product: 16 neighbouring codes are one piece for two steps
   static __device__ __forceinline__ int feature(int st, int half) { return kCodes ? st / 2 * 32 + half * 16 + st % 2 * 8 : st * 16 + half * 8; }
   __device__ __forceinline__ void load_q(const bf16_t* row, int half) {
@@ -111,11 +110,11 @@ struct Operands {
   }
   __device__ __forceinline__ f32x16_t scores(const char* stage, int col, int half, bool drafted) const {
     f32x16_t s = {0};
+    const char* row = stage + col * stage_row(drafted) + feature(0, half) * (codes(drafted) ? 1 : 2);
     if (codes(drafted)) {
-      const unsigned lane_at = col * kD + ((half ^ (col >> 1 & 7)) * 16);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const u32x4_t k = *reinterpret_cast<const u32x4_t*>(stage + (lane_at ^ i * 32));
+        const u32x4_t k = *reinterpret_cast<const u32x4_t*>(row + i * 32);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           Vec8<fp8_t> c;
@@ -124,17 +123,15 @@ struct Operands {
         }
       }
     } else {
-      const unsigned lane_at = col * (2 * kD) + ((feature(0, half) / 8 ^ (col & 15)) * 16);
 #pragma unroll
       for (int st = 0; st < 8; ++st) {
-        const u32x4_t k = *reinterpret_cast<const u32x4_t*>(stage + (lane_at ^ feature(st, 0) * 2));
+        const u32x4_t k = *reinterpret_cast<const u32x4_t*>(row + feature(st, 0) * 2);
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, k), q[st], s, 0, 0, 0);
       }
     }
     return s;
   }
   // lane (n, half): features 4n .. 4n+3 of key row_of(i, half), from memory
-  static constexpr __device__ __forceinline__ unsigned v_bytes(bool drafted) { return codes(drafted) ? 4 : 8; }
   template <bool DRAFTED> __device__ __forceinline__ void load_v(int i, global_t at) {
     if (codes(DRAFTED)) v[i][0] = stream_from<unsigned>(at);
     else v[i] = stream_from<u32x2_t>(at);
@@ -143,9 +140,9 @@ struct Operands {
   __device__ __forceinline__ void stage_v(const char* stage, int col, int half, bool drafted) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int key = row_of(i, half);
-      if (codes(drafted)) v[i][0] = *reinterpret_cast<const unsigned*>(stage + key * kD + (((col >> 2) ^ (key >> 1 & 7)) * 16) + (col & 3) * 4);
-      else v[i] = *reinterpret_cast<const u32x2_t*>(stage + key * (2 * kD) + (((col >> 1) ^ (key & 15)) * 16) + (col & 1) * 8);
+      const char* at = stage + v_offset(i, col, half, drafted, stage_row(drafted));
+      if (codes(drafted)) v[i][0] = *reinterpret_cast<const unsigned*>(at);
+      else v[i] = *reinterpret_cast<const u32x2_t*>(at);
     }
   }
   // codes become bf16 (exact: four significant bits)
@@ -216,32 +213,32 @@ struct Operands<float, PARTS> {
   typedef float Query;
   static constexpr bool kCodes = false;
   typedef __attribute__((ext_vector_type(4))) float f4;
-  static constexpr int kStageBytes = kTile * 4 * kD, kPieces = 16;
+  static constexpr int kStageBytes = kTile * (4 * kD + 16), kPieces = 16;
   f4 q[16], v[16];
   static constexpr __device__ __forceinline__ unsigned row_bytes(bool) { return 4 * kD; }
+  static constexpr __device__ __forceinline__ unsigned stage_row(bool) { return 4 * kD + 16; }
   static constexpr __device__ __forceinline__ int rounds(bool) { return 16; }
-  static __device__ __forceinline__ int key_of(int slot, bool) { return slot >> 5; }
-  static __device__ __forceinline__ int piece_of(int slot, bool) { return (slot & 31) ^ (slot >> 5); }
-  static __device__ __forceinline__ unsigned k_offset(int i, int lane, bool) {
-    return i * 1024 + ((lane >> 5) * (4 * kD) + (((lane & 31) ^ (lane >> 5)) * 16 ^ i * 32));
+  static constexpr __device__ __forceinline__ int key_of(int slot, bool) { return slot >> 5; }
+  static constexpr __device__ __forceinline__ unsigned piece_of(int slot, bool) { return (slot & 31) * 16; }
+  static constexpr __device__ __forceinline__ unsigned v_bytes(bool) { return 16; }
+  static constexpr __device__ __forceinline__ unsigned v_offset(int i, int col, int half, bool, unsigned row) {
+    return row_of(i, 0) * row + (half * 4 * row + col * 16);
   }
-  static __device__ __forceinline__ unsigned v_offset(int i, int col, int half, bool) { return row_of(i, 0) * (4 * kD) + half * 16 * kD + col * 16; }
   __device__ __forceinline__ void load_q(const float* row, int half) {
 #pragma unroll
     for (int st = 0; st < 16; ++st) q[st] = *reinterpret_cast<const f4*>(row + st * 8 + half * 4);
   }
   __device__ __forceinline__ f32x16_t scores(const char* stage, int col, int half, bool) const {
     f32x16_t s = {0};
-    const unsigned lane_at = col * (4 * kD) + ((half ^ col) * 16);
+    const char* row = stage + col * stage_row(false) + half * 16;
 #pragma unroll
     for (int st = 0; st < 16; ++st) {
-      const f4 k = *reinterpret_cast<const f4*>(stage + (lane_at ^ st * 32));
+      const f4 k = *reinterpret_cast<const f4*>(row + st * 32);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], q[st][e], s, 0, 0, 0);
     }
     return s;
   }
-  static constexpr __device__ __forceinline__ unsigned v_bytes(bool) { return 16; }
   template <bool> __device__ __forceinline__ void load_v(int i, global_t at) { v[i] = stream_from<f4>(at); }
   __device__ __forceinline__ void widen_v(bool) {}
   __device__ __forceinline__ unsigned zero_no_numbers() {
@@ -343,7 +340,8 @@ struct Cursor {
   }
 };
 
-template <bool LISTS>
+// SHAPED: scores are capped, biased or cut, here and below.
+template <bool LISTS, bool SHAPED>
 __device__ __forceinline__ Place locate(const TreeParams& p, const Unit& u, const Rows& w, Cursor& c, int t) {
   const int col = threadIdx.x & 31;
   Place at;
@@ -356,7 +354,7 @@ __device__ __forceinline__ Place locate(const TreeParams& p, const Unit& u, cons
     at.last = u.n_drafted - 1;
     at.word = (unsigned)(u.sees >> at.first) & (left >= kTile ? ~0u : (1u << left) - 1u);
     at.row = min(at.first + col, at.last);
-    if (p.slopes) at.pos = u.pos[at.row];
+    if (SHAPED && p.slopes) at.pos = u.pos[at.row];
     return at;
   }
   const int k0 = t * kTile, end = min(k0 + kTile, u.n_keys);
@@ -391,23 +389,25 @@ __device__ __forceinline__ Place locate(const TreeParams& p, const Unit& u, cons
       if (c.j - c.j0 >= 63) c.fill(u, c.j);
     }
     at.one = whole;
-    if (p.slopes || p.starts) at.pos = u.idx[at.row];
+    if (SHAPED && (p.slopes || p.starts)) at.pos = u.idx[at.row];
   }
   return at;
 }
 
 // The scores of a tile become weights: cap, bias, mask, running reference and sum.  -> the keys that the lane's row attends.
+template <bool SHAPED>
 __device__ __forceinline__ unsigned weigh(const TreeParams& p, const Unit& u, Rows& w, const Place& at, f32x16_t& s, int* s_pos, int col,
                                       int half) {
   // Scores times `mult` are in units of log2.  Multiplied beforehand where they are capped or biased, in the last step otherwise.
   const float scale = at.drafted ? p.scale : u.scale;
   float mult = scale * kLog2e;
-  if (p.softcap > 0.f) {
+  const bool biased = SHAPED && p.slopes, cut = SHAPED && p.starts && !at.drafted;
+  if (SHAPED && p.softcap > 0.f) {
     const float to_cap = scale / p.softcap;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = capped(s[r] * to_cap, w.cap2);
     mult = 1.f;
-  } else if (p.slopes || !(mult > 0.f)) {
+  } else if (biased || !(mult > 0.f)) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] *= mult;
     mult = 1.f;
@@ -424,10 +424,10 @@ __device__ __forceinline__ unsigned weigh(const TreeParams& p, const Unit& u, Ro
       f(4 * j + 3, v.w);
     }
   };
-  if (p.slopes || (p.starts && !at.drafted)) {
+  if (biased || cut) {
     s_pos[col] = at.pos;
     wave_lds_fence();
-    if (p.starts && !at.drafted) for_positions([&](int r, int pos) { word &= pos < w.start ? ~(1u << row_of(r, half)) : ~0u; });
+    if (cut) for_positions([&](int r, int pos) { word &= pos < w.start ? ~(1u << row_of(r, half)) : ~0u; });
   }
   if (__ballot(word != ~0u) != 0ull) {
     const unsigned mine = word >> 4 * half;
@@ -441,7 +441,7 @@ __device__ __forceinline__ unsigned weigh(const TreeParams& p, const Unit& u, Ro
   // Scores relative to the row's reference.  The bias of far keys is large, its difference to the reference is not: one fused
   // step takes both, so that nothing of that difference is lost.
   float ref = w.m == kNegBig ? 0.f : w.m, top = -INFINITY;
-  if (p.slopes) {
+  if (biased) {
     for_positions([&](int r, int pos) { top = fmaxf(top, s[r] + fmaf(w.slope2, (float)(pos - w.at_pos), -ref)); });
     top = fmaxf(top, other_half(top));
   } else {
@@ -464,7 +464,7 @@ __device__ __forceinline__ unsigned weigh(const TreeParams& p, const Unit& u, Ro
       for (int e = 0; e < 4; ++e) w.o[e][r] *= a;
     }
   }
-  if (p.slopes) for_positions([&](int r, int pos) { s[r] += fmaf(w.slope2, (float)(pos - w.at_pos), -ref); });
+  if (biased) for_positions([&](int r, int pos) { s[r] += fmaf(w.slope2, (float)(pos - w.at_pos), -ref); });
   else
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], mult, -ref);
@@ -503,13 +503,13 @@ __device__ __forceinline__ void load_keys(u32x4_t (&k)[Op::kPieces], const Place
   if (whole_tile<LISTS>(at)) {
     const global_t tile = base + (size_t)(unsigned)__builtin_amdgcn_readfirstlane(at.first) * Op::row_bytes(DRAFTED);
 #pragma unroll
-    for (int i = 0; i < N; ++i) k[i] = stream_from<u32x4_t>(tile + Op::k_offset(i0 + i, ln, DRAFTED));
+    for (int i = 0; i < N; ++i) k[i] = stream_from<u32x4_t>(tile + (unsigned)((i0 + i) * 64 + ln) * 16);
   } else {
     unsigned row[N];
     rows_of_keys<LISTS>(at, row, [&](int i) { return Op::key_of((i0 + i) * 64 + ln, DRAFTED); });
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      k[i] = stream_from<u32x4_t>(base + (row[i] * Op::row_bytes(DRAFTED) + Op::piece_of((i0 + i) * 64 + ln, DRAFTED) * 16));
+      k[i] = stream_from<u32x4_t>(base + (row[i] * Op::row_bytes(DRAFTED) + Op::piece_of((i0 + i) * 64 + ln, DRAFTED)));
   }
 }
 template <typename Op, bool LISTS, bool DRAFTED>
@@ -518,7 +518,7 @@ __device__ __forceinline__ void load_values(Op& op, const Place& at, global_t ba
   if (whole_tile<LISTS>(at)) {
     const global_t tile = base + (size_t)(unsigned)__builtin_amdgcn_readfirstlane(at.first) * Op::row_bytes(DRAFTED);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) op.template load_v<DRAFTED>(i, tile + Op::v_offset(i, ln & 31, ln >> 5, DRAFTED));
+    for (int i = 0; i < 16; ++i) op.template load_v<DRAFTED>(i, tile + Op::v_offset(i, ln & 31, ln >> 5, DRAFTED, Op::row_bytes(DRAFTED)));
   } else {
     unsigned row[16];
     rows_of_keys<LISTS>(at, row, [&](int i) { return row_of(i, ln >> 5); });
@@ -531,7 +531,7 @@ __device__ __forceinline__ void load_values(Op& op, const Place& at, global_t ba
 // or a NaN is no zero.  `careful`: such values are kept out of the products, and a row that does attend one is marked
 // (row_by_definition computes it).  Drafted tiles are always looked at, since what is not there may hold anything;
 // others when the outputs of a first walk are no numbers.
-template <typename Op, bool LISTS>
+template <typename Op, bool LISTS, bool SHAPED>
 __device__ __forceinline__ void walk(const TreeParams& p, const Unit& u, Op& op, Rows& w, int t0, int t1, char* stage, int* s_pos, bool careful) {
   const int lane = threadIdx.x & 63;
   u32x4_t k[Op::kPieces];
@@ -543,7 +543,7 @@ __device__ __forceinline__ void walk(const TreeParams& p, const Unit& u, Op& op,
   Place at;
   auto seek = [&](Place& to) {                           // the next tile that one of the wave's rows attends
     for (; t < t1; ++t) {
-      to = locate<LISTS>(p, u, w, c, t);
+      to = locate<LISTS, SHAPED>(p, u, w, c, t);
       if (__ballot(to.word != 0u) != 0ull) return true;
     }
     return false;
@@ -563,18 +563,21 @@ __device__ __forceinline__ void walk(const TreeParams& p, const Unit& u, Op& op,
   load_v(at);
   while (true) {
     const int ln = this_lane(), col = ln & 31, half = ln >> 5;
-    auto put = [&](int i0) {
+    auto put = [&](int i0, bool drafted) {
 #pragma unroll
-      for (int i = 0; i < Op::kPieces; ++i) *reinterpret_cast<u32x4_t*>(stage + ((i0 + i) * 64 + ln) * 16) = k[i];
+      for (int i = 0; i < Op::kPieces; ++i) {
+        const int slot = (i0 + i) * 64 + ln;
+        *reinterpret_cast<u32x4_t*>(stage + Op::key_of(slot, drafted) * Op::stage_row(drafted) + Op::piece_of(slot, drafted)) = k[i];
+      }
     };
     if (Op::kCodes && at.drafted) {
 #pragma unroll 1
       for (int i0 = 0; i0 < Op::rounds(true); i0 += Op::kPieces) {
         load_keys<Op, LISTS, true>(k, at, uniform(u.kt), i0);
-        put(i0);
+        put(i0, true);
       }
     } else {
-      put(0);
+      put(0, false);
     }
     wave_lds_fence();
     Place next;
@@ -584,7 +587,7 @@ __device__ __forceinline__ void walk(const TreeParams& p, const Unit& u, Op& op,
     if (more) load_k(next);                              // in flight under everything that follows
     __builtin_amdgcn_sched_barrier(0);
     f32x16_t s = op.scores(stage, col, half, at.drafted);
-    const unsigned attended = weigh(p, u, w, at, s, s_pos, col, half);
+    const unsigned attended = weigh<SHAPED>(p, u, w, at, s, s_pos, col, half);
     if (sizeof(typename Op::Query) == 2 && u.vscale != 1.f && !at.drafted)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] *= u.vscale;
@@ -672,7 +675,7 @@ __device__ __forceinline__ int first_tile(const TreeParams& p, const int* s_star
 }
 
 // What a wave needs of a unit; its rows' queries.
-template <typename C, bool LISTS, typename Op>
+template <typename C, bool LISTS, bool SHAPED, typename Op>
 __device__ __forceinline__ void enter(const TreeParams& p, int unit, int t, int g, int half, Unit& u, Rows& w, Op& op) {
   typedef typename Op::Query Q;
   const int s = unit / p.Hkv, h = unit - s * p.Hkv, hq = h * p.G + g;
@@ -694,18 +697,18 @@ __device__ __forceinline__ void enter(const TreeParams& p, int unit, int t, int 
   u.scale = p.scale * (p.kscale ? p.kscale[unit] : 1.f);
   u.vscale = p.vscale ? p.vscale[unit] : 1.f;
   w.token = t;
-  w.start = p.starts ? p.starts[token] : 0;
-  w.slope2 = p.slopes ? p.slopes[hq] * kLog2e : 0.f;
-  w.at_pos = p.slopes ? u.pos[t] : 0;
+  w.start = SHAPED && p.starts ? p.starts[token] : 0;
+  w.slope2 = SHAPED && p.slopes ? p.slopes[hq] * kLog2e : 0.f;
+  w.at_pos = SHAPED && p.slopes ? u.pos[t] : 0;
   w.cap2 = p.softcap * kLog2e;
 }
 
 // The outputs of a wave's rows go to the partial results of a share; KW waves that walked different tiles for the same rows add
 // theirs up first, a KW-th of the rows each.  Every wave of the workgroup calls it.
-template <int WAVES>
-__device__ __forceinline__ void put_partial(const TreeParams& p, const Rows& w, size_t slot, int left, int RW, int wave, float4* s_o /* [wave][16][64] */,
+template <int WAVES, int kOut /* float4 of a wave, its own until here */>
+__device__ __forceinline__ void put_partial(const TreeParams& p, const Rows& w, size_t slot, int left, int RW, int wave, float4* s_o /* [wave][kOut] */,
                                             float2* s_ml /* [wave][32] */) {
-  constexpr int kOut = 16 * 64;
+  static_assert(kOut >= 16 * 64, "a wave's outputs");
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, KW = WAVES / RW, rw = wave % RW, kp = wave / RW;
   // the sign of a sum says that its row is marked
   const bool marked = (w.marked | __float_as_uint(other_half(__uint_as_float(w.marked)))) != 0u;

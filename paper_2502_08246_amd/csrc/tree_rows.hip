@@ -10,9 +10,9 @@ namespace saap {
 namespace {
 
 constexpr int kWaves = 8;
-constexpr int kTileBytes = 2 * kTile * 2 * kD;           // keys and values of a tile in bf16
+constexpr int kTileBytes = 2 * kTile * (2 * kD + 16);    // keys and values of a tile in bf16
 
-template <typename C, bool LISTS, int PARTS, int RW>
+template <typename C, bool LISTS, bool SHAPED, int PARTS, int RW>
 __global__ void __launch_bounds__(64 * kWaves, 2)
 tree_rows_kernel(TreeParams p) {
   typedef Operands<C, PARTS> Op;
@@ -20,7 +20,7 @@ tree_rows_kernel(TreeParams p) {
   constexpr int kSlots = Op::kCodes ? 256 : 512, kPer = 2 * kSlots / (64 * RW);      // 16-byte pieces of a tile's keys; of a tile to a lane
   extern __shared__ float4 s_all[];
   char* s_stage = reinterpret_cast<char*>(s_all);        // [group][2][TS] tiles; later the waves' outputs
-  static_assert(KW * 2 * TS * kTileBytes == kWaves * 16 * 64 * (int)sizeof(float4), "both in one place");
+  static_assert(KW * 2 * TS * kTileBytes >= kWaves * 16 * 64 * (int)sizeof(float4), "both in one place");
   float2* s_ml = reinterpret_cast<float2*>(s_stage + KW * 2 * TS * kTileBytes);      // [wave][32]
   int* s_pos_all = reinterpret_cast<int*>(s_ml + kWaves * kTile);       // [wave][32]
   int* s_start = s_pos_all + kWaves * kTile;             // [units + 1]
@@ -42,7 +42,7 @@ tree_rows_kernel(TreeParams p) {
     const int n = seg_end - lo, t0 = lo - first + n * kp / KW, t1 = lo - first + n * (kp + 1) / KW;
     const int stages = ((n + KW - 1) / KW + TS - 1) / TS;          // of the group with the most tiles
     Unit u;
-    enter<C, LISTS>(p, unit, token, g, lane >> 5, u, w, op);
+    enter<C, LISTS, SHAPED>(p, unit, token, g, lane >> 5, u, w, op);
     for (bool careful = false;; careful = true) {
       if (tid == 0) s_again = 0;
       w.clear();
@@ -56,7 +56,7 @@ tree_rows_kernel(TreeParams p) {
         for (int j = 0; j < TS; ++j) {
           const int t = t0 + at_stage * TS + j;
           if (t >= t1) continue;
-          const Place at = locate<LISTS>(p, u, w, ahead, t);
+          const Place at = locate<LISTS, SHAPED>(p, u, w, ahead, t);
           if (Op::kCodes && at.drafted) continue;        // twice as long as rows of codes: not fetched ahead
           const int ln = this_lane();
           unsigned row[kPer];
@@ -66,7 +66,7 @@ tree_rows_kernel(TreeParams p) {
             const bool values = (m * RW + rw) * 64 >= kSlots;
             const int slot = ((m * RW + rw) * 64 + ln) & (kSlots - 1);
             const global_t base = at.drafted ? values ? uniform(u.vt) : uniform(u.kt) : values ? uniform(u.V) : uniform(u.K);
-            piece[j * kPer + m] = stream_from<u32x4_t>(base + (row[m] * Op::row_bytes(false) + Op::piece_of(slot, false) * 16));
+            piece[j * kPer + m] = stream_from<u32x4_t>(base + (row[m] * Op::row_bytes(false) + Op::piece_of(slot, false)));
           }
         }
       };
@@ -78,24 +78,27 @@ tree_rows_kernel(TreeParams p) {
           const int t = t0 + at_stage * TS + j;
           if (t >= t1) continue;
           if (Op::kCodes && t >= u.key_tiles) {
-            const Place at = locate<LISTS>(p, u, w, ahead, t);
+            const Place at = locate<LISTS, SHAPED>(p, u, w, ahead, t);
 #pragma unroll 1
             for (int m = 0; m < 1024 / (64 * RW); ++m) {
               const int all = (m * RW + rw) * 64 + ln, slot = all & 511;
               const global_t base = (m * RW + rw) * 64 >= 512 ? uniform(u.vt) : uniform(u.kt);
               const unsigned row = (unsigned)row_of_key<false>(at, Op::key_of(slot, true));
-              *reinterpret_cast<u32x4_t*>(to + j * kTileBytes + all * 16) =
-                  stream_from<u32x4_t>(base + (row * Op::row_bytes(true) + Op::piece_of(slot, true) * 16));
+              *reinterpret_cast<u32x4_t*>(to + j * kTileBytes + Op::key_of(all, true) * Op::stage_row(true) + Op::piece_of(slot, true)) =
+                  stream_from<u32x4_t>(base + (row * Op::row_bytes(true) + Op::piece_of(slot, true)));
             }
           } else {
 #pragma unroll
-            for (int m = 0; m < kPer; ++m)
-              *reinterpret_cast<u32x4_t*>(to + j * kTileBytes + ((m * RW + rw) * 64 + ln) * 16) = piece[j * kPer + m];
+            for (int m = 0; m < kPer; ++m) {
+              const int slot = (m * RW + rw) * 64 + ln;  // keys, then values
+              *reinterpret_cast<u32x4_t*>(to + j * kTileBytes + Op::key_of(slot, false) * Op::stage_row(false) + Op::piece_of(slot, false)) =
+                  piece[j * kPer + m];
+            }
           }
         }
       };
       Place next;
-      if (t0 < t1) next = locate<LISTS>(p, u, w, c, t0);
+      if (t0 < t1) next = locate<LISTS, SHAPED>(p, u, w, c, t0);
       fetch(0);
       put(0);
       fetch(1);
@@ -107,16 +110,16 @@ tree_rows_kernel(TreeParams p) {
           const int t = t0 + i * TS + j;
           if (t >= t1) break;
           const Place at = next;
-          if (t + 1 < t1) next = locate<LISTS>(p, u, w, c, t + 1);
+          if (t + 1 < t1) next = locate<LISTS, SHAPED>(p, u, w, c, t + 1);
           if (__ballot(at.word != 0u) == 0ull) continue; // none of the wave's rows attends it
           const char* tile = stage + ((i & 1) * TS + j) * kTileBytes;
           const int ln = this_lane(), col = ln & 31, half = ln >> 5;
           f32x16_t s = op.scores(tile, col, half, at.drafted);
-          const unsigned attended = weigh(p, u, w, at, s, s_pos, col, half);
+          const unsigned attended = weigh<SHAPED>(p, u, w, at, s, s_pos, col, half);
           if (u.vscale != 1.f && !at.drafted)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] *= u.vscale;
-          op.stage_v(tile + (Op::kCodes && !at.drafted ? 256 : 512) * 16, col, half, at.drafted);
+          op.stage_v(tile + kTile * Op::stage_row(at.drafted), col, half, at.drafted);
           op.widen_v(at.drafted);
           if (careful || at.drafted) w.marked |= op.zero_no_numbers() & attended;
           op.add(w.o, s);
@@ -134,33 +137,34 @@ tree_rows_kernel(TreeParams p) {
       __syncthreads();
       if (careful || !again) break;
     }
-    put_partial<kWaves>(p, w, ((size_t)blockIdx.x + unit) * p.R + row0, left, RW, wave, reinterpret_cast<float4*>(s_stage), s_ml);
+    put_partial<kWaves, 16 * 64>(p, w, ((size_t)blockIdx.x + unit) * p.R + row0, left, RW, wave, reinterpret_cast<float4*>(s_stage), s_ml);
     lo = seg_end;
   }
 }
 
-template <typename C, bool LISTS, int PARTS, int RW>
+template <typename C, bool LISTS, bool SHAPED, int PARTS, int RW>
 bool launch(const TreeParams& p, int blocks, hipStream_t hs) {
-  const size_t lds = (size_t)kWaves * 16 * 64 * sizeof(float4) + sizeof(float2) * kWaves * kTile + sizeof(int) * (kWaves * kTile + p.units + 1);
-  if (!allow_lds<tree_rows_kernel<C, LISTS, PARTS, RW>>(lds)) return false;
-  hipLaunchKernelGGL((tree_rows_kernel<C, LISTS, PARTS, RW>), dim3((unsigned)p.shares, (unsigned)blocks), dim3(64 * kWaves), lds, hs, p);
+  const size_t lds = (size_t)8 * kTileBytes + sizeof(float2) * kWaves * kTile + sizeof(int) * (kWaves * kTile + p.units + 1);
+  if (!allow_lds<tree_rows_kernel<C, LISTS, SHAPED, PARTS, RW>>(lds)) return false;
+  hipLaunchKernelGGL((tree_rows_kernel<C, LISTS, SHAPED, PARTS, RW>), dim3((unsigned)p.shares, (unsigned)blocks), dim3(64 * kWaves), lds, hs, p);
   return true;
 }
-template <typename C, bool LISTS, int PARTS>
+template <typename C, bool LISTS, bool SHAPED, int PARTS>
 bool launch(const TreeParams& p, int blocks, hipStream_t hs) {
-  if (p.RW == 2) return launch<C, LISTS, PARTS, 2>(p, blocks, hs);
-  return p.RW == 4 ? launch<C, LISTS, PARTS, 4>(p, blocks, hs) : launch<C, LISTS, PARTS, 8>(p, blocks, hs);
+  if (p.RW == 2) return launch<C, LISTS, SHAPED, PARTS, 2>(p, blocks, hs);
+  return p.RW == 4 ? launch<C, LISTS, SHAPED, PARTS, 4>(p, blocks, hs) : launch<C, LISTS, SHAPED, PARTS, 8>(p, blocks, hs);
 }
-template <typename C>
+template <typename C, int PARTS>
 bool launch(const TreeParams& p, int blocks, bool lists, hipStream_t hs) {
-  if (p.out_bf16) return lists ? launch<C, true, 2>(p, blocks, hs) : launch<C, false, 2>(p, blocks, hs);
-  return lists ? launch<C, true, 3>(p, blocks, hs) : launch<C, false, 3>(p, blocks, hs);
+  if (shaped(p)) return lists ? launch<C, true, true, PARTS>(p, blocks, hs) : launch<C, false, true, PARTS>(p, blocks, hs);
+  return lists ? launch<C, true, false, PARTS>(p, blocks, hs) : launch<C, false, false, PARTS>(p, blocks, hs);
 }
 
 }  // namespace
 
 bool launch_tree_rows(const TreeParams& p, int blocks, bool codes, bool lists, hipStream_t hs) {
-  return codes ? launch<fp8_t>(p, blocks, lists, hs) : launch<bf16_t>(p, blocks, lists, hs);
+  if (codes) return p.out_bf16 ? launch<fp8_t, 2>(p, blocks, lists, hs) : launch<fp8_t, 3>(p, blocks, lists, hs);
+  return p.out_bf16 ? launch<bf16_t, 2>(p, blocks, lists, hs) : launch<bf16_t, 3>(p, blocks, lists, hs);
 }
 
 }  // namespace saap
