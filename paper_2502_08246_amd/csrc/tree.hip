@@ -84,46 +84,7 @@ tree_plan_kernel(TreeParams p) {
   }
 }
 
-// A workgroup's share, RW waves with rows of their own, KW of each that share out the tiles of a unit.
-template <typename C, bool LISTS, bool SHAPED, int PARTS>
-__global__ void __launch_bounds__(64 * kWaves, sizeof(C) == 4 ? 1 : 2)
-tree_attend_kernel(TreeParams p) {
-  typedef Operands<C, PARTS> Op;
-  extern __shared__ float4 s_all[];
-  float4* s_o = s_all;                                   // [wave][kWaveLds]: the wave's stage, then its outputs
-  float2* s_ml = reinterpret_cast<float2*>(s_o + kWaves * kWaveLds);    // [wave][32]
-  int* s_pos_all = reinterpret_cast<int*>(s_ml + kWaves * kTile);       // [wave][32]
-  int* s_start = s_pos_all + kWaves * kTile;             // [units + 1]
-  __shared__ int s_sum[kWaves];
-  static_assert(Op::kStageBytes <= kWaveLds * (int)sizeof(float4) && kWaveLds >= 16 * 64, "a stage or its outputs in the wave's part");
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
-  const Share mine = find_share(p, s_start, s_sum, kWaves);
-  if (!mine.there) return;
-  const int RW = p.RW, KW = kWaves / RW, rw = wave % RW, kp = wave / RW;
-  const int row0 = (blockIdx.y * RW + rw) * kTile, row = min(row0 + col, p.R - 1), left = p.R - row0;
-  const int t = row / p.G, g = row - t * p.G;
-  Op op;
-  Rows w;
-  int lo = mine.lo;
-  for (int unit = mine.unit; lo < mine.hi; ++unit) {
-    const int first = first_tile(p, s_start, unit), seg_end = min(mine.hi, first_tile(p, s_start, unit + 1));
-    if (seg_end <= lo) continue;                         // a unit without tiles
-    const int n = seg_end - lo, t0 = lo - first + n * kp / KW, t1 = lo - first + n * (kp + 1) / KW;
-    Unit u;
-    enter<C, LISTS, SHAPED>(p, unit, t, g, half, u, w, op);
-    char* stage = reinterpret_cast<char*>(s_o + wave * kWaveLds);
-    int* s_pos = s_pos_all + wave * kTile;
-    const size_t slot = ((size_t)blockIdx.x + unit) * p.R + row0;
-    for (bool careful = false;; careful = true) {
-      walk<Op, LISTS, SHAPED>(p, u, op, w, t0, t1, stage, s_pos, careful);
-      if (careful || !w.has_no_numbers()) break;
-    }
-    put_partial<kWaves, kWaveLds>(p, w, slot, left, RW, wave, s_o, s_ml);
-    lo = seg_end;
-  }
-}
-
-// ---- 3. the shares of a row ------------------------------------------------------------------------------------------------------
+// ---- 2. the shares of a unit ---------------------------------------------------------------------------------------------------
 // Element e of a row of the cache or of the drafted rows.
 template <typename C> __device__ __forceinline__ float element(const char* row, int e) {
   if constexpr (sizeof(C) == 1) return __builtin_amdgcn_cvt_f32_fp8((int)reinterpret_cast<const uint8_t*>(row)[e], 0);
@@ -133,14 +94,25 @@ template <typename C> __device__ __forceinline__ float element(const char* row, 
 // A row that attends infinities or NaN: computed from the definition, key by key.  Ordinary values never
 // come here.  -> the output's feature `tid` (tid < 128).
 template <typename C>
-__device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit, int row, float* s_w /* 256 */, float* s_red /* 8 */) {
+__device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit, int row, int n_runs, int n_keys, float* s_w /* 256 */,
+                                                  float* s_red /* 8 */, const int4* runs /* p.listed */) {
   typedef typename DotType<C>::type Q;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int s = unit / p.Hkv, h = unit - s * p.Hkv, t = row / p.G, hq = h * p.G + row - t * p.G;
   const size_t token = (size_t)s * p.T + t;
   const char* q = static_cast<const char*>(p.q) + (token * p.Hq + hq) * (kD * sizeof(Q));
-  const int n_keys = keys_of_unit(p, unit), n = n_keys + (p.kt ? p.T : 0), n_runs = p.unit ? p.unit[unit].x : 0;
-  const int4* table = p.table + (size_t)unit * p.cap;
+  const int n = n_keys + (p.kt ? p.T : 0);
+  const bool lists = p.listed || p.unit;
+  // the row of the cache that holds a key of the lists, and whether the row's token lists it
+  auto row_of_key = [&](int key, bool& in) {
+    const int4* table = p.listed ? runs : p.table + (size_t)unit * p.cap;
+    int j = 0;
+    for (int step = 1 << 13; step > 0; step >>= 1)
+      if (j + step < n_runs && table[j + step].x <= key) j += step;
+    const int4 e = table[j];
+    in = ((unsigned)(t < 32 ? e.z : e.w) >> (t & 31)) & 1u;
+    return min(e.y + key - e.x, p.rows - 1);
+  };
   float M = kNegBig, L = 0.f, acc = 0.f;
   for (int base = 0; base < n; base += 256) {
     // a thread to a key
@@ -156,16 +128,9 @@ __device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit
       if (p.slopes) pos = p.pos[(size_t)s * p.T + j];
     } else if (in) {
       int r = key;
-      if (p.unit) {
-        int j = 0;
-        for (int step = 1 << 13; step > 0; step >>= 1)
-          if (j + step < n_runs && table[j + step].x <= key) j += step;
-        const int4 e = table[j];
-        r = min(e.y + key - e.x, p.rows - 1);
-        in = ((unsigned)(t < 32 ? e.z : e.w) >> (t & 31)) & 1u;
-      }
+      if (lists) r = row_of_key(key, in);
       at = (size_t)unit * p.rows + r;
-      pos = p.unit ? (p.idx ? p.idx[at] : 0) : r;
+      pos = lists ? (p.idx ? p.idx[at] : 0) : r;
       if (p.starts) in = in && pos >= p.starts[token];
     }
     float a = -INFINITY;
@@ -199,12 +164,8 @@ __device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit
           v = element<Q>(static_cast<const char*>(p.vt) + ((size_t)unit * p.T + key_i - n_keys) * (kD * sizeof(Q)), tid);
         } else {
           int r = key_i;
-          if (p.unit) {
-            int j = 0;
-            for (int step = 1 << 13; step > 0; step >>= 1)
-              if (j + step < n_runs && table[j + step].x <= key_i) j += step;
-            r = min(table[j].y + key_i - table[j].x, p.rows - 1);
-          }
+          bool in_list;
+          if (lists) r = row_of_key(key_i, in_list);
           v = element<C>(static_cast<const char*>(p.V) + ((size_t)unit * p.rows + r) * (kD * sizeof(C)), tid) * (p.vscale ? p.vscale[unit] : 1.f);
         }
         acc = fmaf(s_w[i], v, acc);
@@ -214,6 +175,120 @@ __device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit
   return L == 0.f ? 0.f : acc / L;
 }
 
+// A row's output, feature 4 c .. 4 c + 3 in lane c of 32, and its lse.
+__device__ __forceinline__ size_t place_of_row(const TreeParams& p, int unit, int row) {
+  const int s = unit / p.Hkv, h = unit - s * p.Hkv, t = row / p.G, g = row - t * p.G;
+  return (size_t)(s * p.T + t) * p.Hq + h * p.G + g;
+}
+__device__ __forceinline__ void put_output(const TreeParams& p, size_t to, int c, const float4& o, float M, float L) {
+  const float inv = L == 0.f ? 0.f : 1.0f / L;           // no key: zeros
+  if (p.out_bf16)
+    *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + to * kD + 4 * c) =
+        make_uint2(pack_bf16(o.x * inv, o.y * inv), pack_bf16(o.z * inv, o.w * inv));
+  else
+    *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to * kD + 4 * c) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  if (c == 0 && p.lse) p.lse[to] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
+}
+template <typename C>
+__device__ __forceinline__ void redo_row(const TreeParams& p, int unit, int row, int n_runs, int n_keys, float* s_w, float* s_red, const int4* runs) {
+  const float o = row_by_definition<C>(p, unit, row, n_runs, n_keys, s_w, s_red, runs);
+  const size_t to = place_of_row(p, unit, row);
+  if (threadIdx.x < kD) {
+    if (p.out_bf16) static_cast<bf16_t*>(p.out)[to * kD + threadIdx.x] = (bf16_t)(pack_bf16(o, o) & 0xffffu);
+    else static_cast<float*>(p.out)[to * kD + threadIdx.x] = o;
+  }
+}
+
+// A workgroup's share, RW waves with rows of their own, KW of each that share out its tiles.
+template <typename C, bool LISTS, bool SHAPED, int PARTS>
+__global__ void __launch_bounds__(64 * kWaves, sizeof(C) == 4 ? 1 : 2)
+tree_attend_kernel(TreeParams p) {
+  typedef Operands<C, PARTS> Op;
+  extern __shared__ float4 s_all[];
+  float4* s_o = s_all;                                   // [wave][kWaveLds]: the wave's stage, then its outputs
+  float2* s_ml = reinterpret_cast<float2*>(s_o + kWaves * kWaveLds);    // [wave][32]
+  int* s_pos_all = reinterpret_cast<int*>(s_ml + kWaves * kTile);       // [wave][32]
+  static_assert(Op::kStageBytes <= kWaveLds * (int)sizeof(float4) && kWaveLds >= 16 * 64, "a stage or its outputs in the wave's part");
+  touch_arguments(p);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+  Cursor begin;
+  begin.j = begin.j0 = 0;
+  const Share mine = find_share(p, begin);
+  if (!mine.there) return;
+  const int RW = p.RW, KW = kWaves / RW, rw = wave % RW, kp = wave / RW;
+  const int row0 = (blockIdx.y * RW + rw) * kTile, row = min(row0 + col, p.R - 1), left = p.R - row0;
+  const int t = row / p.G, g = row - t * p.G;
+  Op op;
+  Rows w;
+  Unit u;
+  enter<C, SHAPED>(p, mine, t, g, half, u, w, op);
+  const int n = mine.hi - mine.lo, t0 = mine.lo + n * kp / KW, t1 = mine.lo + n * (kp + 1) / KW;
+  char* stage = reinterpret_cast<char*>(s_o + wave * kWaveLds);
+  for (bool careful = false;; careful = true) {
+    walk<Op, LISTS, SHAPED>(p, u, op, w, begin, t0, t1, stage, s_pos_all + wave * kTile, careful);
+    if (careful || !w.has_no_numbers()) break;
+  }
+  put_partial<kWaves, kWaveLds>(p, w, (size_t)mine.slot * p.R + row0, left, RW, wave, s_o, s_ml);
+  if (!p.merged) return;
+
+  // The unit's last share adds them up: a wave to a row, 32 lanes to the features, the halves take the shares in turn.
+  __shared__ int s_last;
+  __shared__ unsigned s_no[64 * 8 / 32];                 // rows that attend values that are no numbers
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // every wave's partial results are out
+  __syncthreads();
+  if (tid == 0) {
+    const unsigned old = __hip_atomic_fetch_add(p.counters + mine.unit, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    s_last = old == (unsigned)(mine.of - 1);
+    if (s_last) __hip_atomic_store(p.counters + mine.unit, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  if (tid < 16) s_no[tid] = 0u;
+  __syncthreads();
+  if (!s_last) return;
+  const size_t slot0 = (size_t)p.per_unit * mine.unit;   // units with even shares only
+  for (int r = wave; r < p.R; r += kWaves) {
+    // lane i: factor of share i (up to 64 of them)
+    const unsigned long long ml = get_far(p.part_ml + (slot0 + min(lane, mine.of - 1)) * p.R + r);
+    const float m = lane < mine.of ? low(ml) : kNegBig, M = wave_max(m), f = lane < mine.of ? fast_exp2(m - M) : 0.f;
+    const float L = wave_sum(lane < mine.of ? f * fabsf(high(ml)) : 0.f);
+    bool no = __ballot(lane < mine.of && (__float_as_uint(high(ml)) >> 31)) != 0ull;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int kDeep = 8;
+    for (int i0 = 0; i0 < mine.of; i0 += 2 * kDeep) {
+      unsigned long long a[kDeep], b[kDeep];
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k) {
+        const float* from = p.part_o + ((slot0 + min(i0 + 2 * k + half, mine.of - 1)) * p.R + r) * kD + 4 * col;
+        a[k] = get_far(from);
+        b[k] = get_far(from + 2);
+      }
+#pragma unroll
+      for (int k = 0; k < kDeep; ++k) {
+        const int i = i0 + 2 * k + half;
+        const float fk = __shfl(f, i & 63);
+        if (i < mine.of) {
+          o.x = fmaf(fk, low(a[k]), o.x); o.y = fmaf(fk, high(a[k]), o.y);
+          o.z = fmaf(fk, low(b[k]), o.z); o.w = fmaf(fk, high(b[k]), o.w);
+        }
+      }
+    }
+    o.x += other_half(o.x); o.y += other_half(o.y); o.z += other_half(o.z); o.w += other_half(o.w);
+    if (half == 0) put_output(p, place_of_row(p, mine.unit, r), col, o, M, L);
+    no |= __ballot(no_number(o.x) | no_number(o.y) | no_number(o.z) | no_number(o.w) | no_number(L)) != 0ull;
+    if (no && lane == 0) atomicOr(&s_no[r >> 5], 1u << (r & 31));
+  }
+  __syncthreads();
+  for (int r = 0; r < p.R; ++r)
+    if (__builtin_expect(s_no[r >> 5] >> (r & 31) & 1u, 0)) {
+      // a list that was taken as it is goes to memory for the rows' threads
+      int4* runs = reinterpret_cast<int4*>(s_o + 512);
+      __syncthreads();
+      if (wave == 0) runs[lane] = begin.e;
+      __syncthreads();
+      redo_row<C>(p, mine.unit, r, mine.n_runs, mine.n_keys, reinterpret_cast<float*>(s_o), reinterpret_cast<float*>(s_o + 256), runs);
+    }
+}
+
+// ---- 3. the shares of a row ------------------------------------------------------------------------------------------------------
 // A workgroup per (unit, row): 32 lanes to the features, eight groups take the shares in turn.
 template <typename C>
 __global__ void __launch_bounds__(256)
@@ -223,13 +298,9 @@ tree_merge_kernel(TreeParams p) {
   __shared__ float4 s_acc[256];
   __shared__ int s_no;
   const int unit = blockIdx.x, row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const bool same = same_units(p);
-  const int one = same ? tiles_of_unit(p, 0) : 0;
-  const long long tiles = same ? one * p.units : p.start[p.units];
-  const int first = same ? unit * one : p.start[unit], end = same ? first + one : p.start[unit + 1], used = shares_used(p, tiles);
-  const int w0 = end > first ? (int)(((long long)(first + 1) * used - 1) / tiles) : 0;
-  const int n = end > first ? (int)(((long long)end * used - 1) / tiles) - w0 + 1 : 0;
-  const size_t slot0 = (size_t)(w0 + unit);
+  const int2 shares = p.start[unit];
+  const int n = shares.y;
+  const size_t slot0 = (size_t)shares.x;
   if (tid == 0) s_no = 0;
   float M = kNegBig;
   for (int i = tid; i < n; i += 256) M = fmaxf(M, p.part_ml[(slot0 + i) * p.R + row].x);
@@ -259,8 +330,6 @@ tree_merge_kernel(TreeParams p) {
   }
   s_acc[tid] = acc;
   __syncthreads();
-  const int s = unit / p.Hkv, h = unit - s * p.Hkv, t = row / p.G, g = row - t * p.G;
-  const size_t to = (size_t)(s * p.T + t) * p.Hq + h * p.G + g;
   if (wave == 0) {
     if (grp == 0) {
 #pragma unroll
@@ -268,13 +337,7 @@ tree_merge_kernel(TreeParams p) {
         const float4 v = s_acc[i * 32 + tid];
         acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
       }
-      const float inv = L == 0.f ? 0.f : 1.0f / L;       // no key: zeros
-      if (p.out_bf16)
-        *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.out) + to * kD + 4 * c) =
-            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-      else
-        *reinterpret_cast<float4*>(static_cast<float*>(p.out) + to * kD + 4 * c) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-      if (tid == 0 && p.lse) p.lse[to] = L == 0.f ? -INFINITY : (M + __log2f(L)) * kLn2;
+      put_output(p, place_of_row(p, unit, row), c, acc, M, L);
     }
     const bool no = no_number(acc.x) | no_number(acc.y) | no_number(acc.z) | no_number(acc.w) | no_number(L);
     const unsigned long long any = __ballot(grp == 0 && no);
@@ -282,18 +345,22 @@ tree_merge_kernel(TreeParams p) {
   }
   __syncthreads();
   if (__builtin_expect(s_no == 0, 1)) return;
-  const float o = row_by_definition<C>(p, unit, row, reinterpret_cast<float*>(s_acc), s_red);
-  if (tid < kD) {
-    if (p.out_bf16) static_cast<bf16_t*>(p.out)[to * kD + tid] = (bf16_t)(pack_bf16(o, o) & 0xffffu);
-    else static_cast<float*>(p.out)[to * kD + tid] = o;
-  }
+  // a list that was taken as it is: once more
+  Cursor list;
+  const int n_keys = p.listed ? take_list(p, unit, list) : keys_of_unit(p, unit);
+  const int n_runs = p.listed ? p.nprobe + (p.resident >= 0 ? 1 : 0) : p.unit ? p.unit[unit].x : 0;
+  int4* runs = reinterpret_cast<int4*>(s_f);
+  __syncthreads();
+  if (p.listed && wave == 0) runs[lane] = list.e;
+  __syncthreads();
+  redo_row<C>(p, unit, row, n_runs, n_keys, reinterpret_cast<float*>(s_acc), s_red, runs);
 }
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // How the rows are laid on waves: waves with rows of their own in a workgroup, workgroups to cover the rows, shares of the keys.
 struct Layout {
-  int RW, blocks, shares, cap, min_tiles;
+  int RW, blocks, shares, grid, cap, min_tiles;
   bool staged;                                           // tree_rows.hip
   size_t start, unit, table, ml, o, bytes;               // offsets in the workspace
   Layout(long long units, int R, int runs, int n_list, bool f32) {
@@ -310,21 +377,23 @@ struct Layout {
     const int fit = (staged || f32 ? 1 : 2) * device_cus() / blocks;
     shares = fit < 1 ? 1 : fit > kMaxShares ? kMaxShares : fit;
     min_tiles = staged ? 8 : 2 * kWaves / RW;
+    // as many shares as there are workgroups at a time, or one to a unit; as many to every unit where they are alike
+    grid = shares > units ? shares : (int)units;
     cap = (runs < n_list + 1 ? runs : n_list + 1) + 1;
     start = SAAP_WS_HEADER_BYTES;
-    unit = start + align256((size_t)(units + 1) * sizeof(int));
+    unit = start + align256((size_t)units * sizeof(int2));
     table = unit + align256((size_t)units * sizeof(int2));
     ml = table + align256(runs > 0 ? (size_t)units * cap * sizeof(int4) : 0);
-    o = ml + align256((size_t)(shares + units) * R * sizeof(float2));
-    bytes = o + (size_t)(shares + units) * R * kD * sizeof(float);
+    o = ml + align256((size_t)grid * R * sizeof(float2));
+    bytes = o + (size_t)grid * R * kD * sizeof(float);
   }
 };
 
 template <typename C, bool LISTS, bool SHAPED, int PARTS>
 bool launch_attend(const TreeParams& p, int blocks, hipStream_t hs) {
-  const size_t lds = sizeof(float4) * kWaves * kWaveLds + sizeof(float2) * kWaves * kTile + sizeof(int) * (kWaves * kTile + p.units + 1);
+  const size_t lds = sizeof(float4) * kWaves * kWaveLds + sizeof(float2) * kWaves * kTile + sizeof(int) * kWaves * kTile;
   if (!allow_lds<tree_attend_kernel<C, LISTS, SHAPED, PARTS>>(lds)) return false;
-  hipLaunchKernelGGL((tree_attend_kernel<C, LISTS, SHAPED, PARTS>), dim3((unsigned)p.shares, (unsigned)blocks), dim3(64 * kWaves), lds, hs, p);
+  hipLaunchKernelGGL((tree_attend_kernel<C, LISTS, SHAPED, PARTS>), dim3((unsigned)p.grid, (unsigned)blocks), dim3(64 * kWaves), lds, hs, p);
   return true;
 }
 template <typename C, int PARTS>
@@ -370,16 +439,33 @@ int32_t attend(const saap_tree* a, const void* q, const void* K, const void* V, 
   p.tree = reinterpret_cast<const long long*>(a->tree); p.off = off; p.len = len; p.idx = a->idx; p.selected = selected; p.n_keys = n_keys;
   p.slopes = a->slopes; p.pos = a->pos; p.starts = a->starts; p.out = out; p.lse = lse;
   char* base = static_cast<char*>(ws);
-  p.start = reinterpret_cast<int*>(base + at.start);
-  p.unit = lists ? reinterpret_cast<int2*>(base + at.unit) : nullptr;
+  p.counters = reinterpret_cast<unsigned*>(base);
+  p.start = reinterpret_cast<int2*>(base + at.start);
   p.table = reinterpret_cast<int4*>(base + at.table);
   p.part_ml = reinterpret_cast<float2*>(base + at.ml);
   p.part_o = reinterpret_cast<float*>(base + at.o);
   p.S = a->S; p.T = a->T; p.Hq = a->Hq; p.Hkv = a->Hkv; p.G = G; p.R = R; p.rows = rows; p.runs = runs; p.nprobe = nprobe;
   p.lists = lists_per_token ? a->T : 1; p.resident = resident_run; p.cap = at.cap; p.shares = at.shares; p.units = (int)units;
   p.out_bf16 = out_dtype == SAAP_BF16; p.RW = at.RW; p.min_tiles = at.min_tiles; p.scale = a->scale; p.softcap = a->softcap;
+  // One list to a unit, short enough for the lanes of a wave: nothing to plan.  Such lists, and dense caches of one length, have
+  // about as many keys each: every unit has as many shares.
+  p.listed = lists && p.lists == 1 && nprobe + (resident_run >= 0 ? 1 : 0) <= 63;
+  p.unit = lists && !p.listed ? reinterpret_cast<int2*>(base + at.unit) : nullptr;
+  p.grid = at.grid;
+  if (p.listed || (!lists && !n_keys)) {
+    p.per_unit = at.shares > units ? (int)(at.shares / units) : 1;
+    if (!lists) {
+      // dense: no more than there are
+      const int tiles = (rows + kTile - 1) / kTile + (a->k_tree ? (a->T + kTile - 1) / kTile : 0), most = (tiles + p.min_tiles - 1) / p.min_tiles;
+      if (most < p.per_unit) p.per_unit = most;
+    }
+    p.grid = (int)(units * p.per_unit);
+    // A unit's last share adds up to 64 of them (a lane each) for one or two rows to a wave sooner than another launch would: 4
+    // rows 27.7 us against 38; for eight rows to a wave, each on its way to memory and back, it takes longer (12 us more).
+    p.merged = !at.staged && R <= 2 * kWaves && p.per_unit <= 64;
+  }
   hipStream_t hs = static_cast<hipStream_t>(stream);
-  if (lists) {
+  if (p.unit) {
     const size_t lds = (size_t)runs * sizeof(unsigned long long);
     if (!allow_lds<tree_plan_kernel>(lds)) return SAAP_HIP_ERROR;
     hipLaunchKernelGGL(tree_plan_kernel, dim3((unsigned)units), dim3(kPlanThreads), lds, hs, p);
@@ -388,6 +474,7 @@ int32_t attend(const saap_tree* a, const void* q, const void* K, const void* V, 
                   : type == CacheType::kF32 ? launch_attend<float>(p, at.blocks, lists, hs)
                   : type == CacheType::kBf16 ? launch_attend<bf16_t>(p, at.blocks, lists, hs) : launch_attend<fp8_t>(p, at.blocks, lists, hs);
   if (!ok) return SAAP_HIP_ERROR;
+  if (p.merged) return launch_status();
   const dim3 merge_grid((unsigned)units, (unsigned)R);
   if (type == CacheType::kF32) hipLaunchKernelGGL(tree_merge_kernel<float>, merge_grid, dim3(256), 0, hs, p);
   else if (type == CacheType::kBf16) hipLaunchKernelGGL(tree_merge_kernel<bf16_t>, merge_grid, dim3(256), 0, hs, p);

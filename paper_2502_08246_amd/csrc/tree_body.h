@@ -20,14 +20,19 @@ struct TreeParams {
   const int32_t *pos, *starts;        // [S,T]
   void* out;
   float* lse;
-  int2* unit;                         // lists: {runs, keys} of a unit
-  int* start;                         // [units + 1]: a unit's first tile on the line
+  int2* unit;                         // planned lists: {runs, keys} of a unit
+  int2* start;                        // [units]: a unit's first share and how many it has
   int4* table;                        // [units][cap]: {place of the first key, first row, tokens 0..31, tokens 32..63}, and the end
-  float2* part_ml;                    // [shares + units][R]
-  float* part_o;                      // [shares + units][R][d]
-  int S, T, Hq, Hkv, G, R, rows, runs, nprobe, lists, resident, cap, shares, units, out_bf16;
+  unsigned* counters;                 // [units]: zero on entry and on exit
+  float2* part_ml;                    // [shares][R]
+  float* part_o;                      // [shares][R][d]
+  int S, T, Hq, Hkv, G, R, rows, runs, nprobe, lists, resident, cap, units, out_bf16;
+  int shares, grid;                   // workgroups that the device holds at a time; workgroups of the launch
+  int per_unit;                       // > 0: every unit has this many shares, whether it fills them or not
   int RW;                             // waves of a workgroup that have rows of their own; the others share out the keys
   int min_tiles;                      // of a share: fewer are not worth its partial results
+  int listed;                         // a list of up to 63 runs to a unit, taken as it is: no plan
+  int merged;                         // a unit's last share adds them up: no merge
   float scale, softcap;
 };
 
@@ -323,8 +328,12 @@ struct Cursor {
     e = u.table[min(from + (int)(threadIdx.x & 63), u.n_runs)];
   }
   // the run that holds key `key`: 64 probes a step
-  __device__ __forceinline__ void find(const Unit& u, int key) {
+  __device__ __forceinline__ void find(const TreeParams& p, const Unit& u, int key) {
     const int lane = threadIdx.x & 63;
+    if (p.listed) {                                      // all of them are there (of empty runs the last begins where the next does)
+      j = max(__popcll(__ballot(e.x <= key && lane < u.n_runs)) - 1, 0);
+      return;
+    }
     int lo = 0, n = u.n_runs;                            // the answer is in [lo, lo + n)
     while (n > 63) {
       const int step = (n + 63) / 64;
@@ -532,14 +541,14 @@ __device__ __forceinline__ void load_values(Op& op, const Place& at, global_t ba
 // (row_by_definition computes it).  Drafted tiles are always looked at, since what is not there may hold anything;
 // others when the outputs of a first walk are no numbers.
 template <typename Op, bool LISTS, bool SHAPED>
-__device__ __forceinline__ void walk(const TreeParams& p, const Unit& u, Op& op, Rows& w, int t0, int t1, char* stage, int* s_pos, bool careful) {
+__device__ __forceinline__ void walk(const TreeParams& p, const Unit& u, Op& op, Rows& w, const Cursor& at_start, int t0, int t1, char* stage, int* s_pos,
+                                     bool careful) {
   const int lane = threadIdx.x & 63;
   u32x4_t k[Op::kPieces];
   w.clear();
-  Cursor c;
-  c.j = c.j0 = 0;
+  Cursor c = at_start;
   int t = t0;
-  if (LISTS && t0 < min(t1, u.key_tiles)) c.find(u, t0 * kTile);
+  if (LISTS && t0 < min(t1, u.key_tiles)) c.find(p, u, t0 * kTile);
   Place at;
   auto seek = [&](Place& to) {                           // the next tile that one of the wave's rows attends
     for (; t < t1; ++t) {
@@ -604,81 +613,114 @@ __device__ __forceinline__ void walk(const TreeParams& p, const Unit& u, Op& op,
   }
 }
 
-// Tiles of a unit's keys and drafted keys on the line.
+// Every line of the kernel's arguments is asked for at once: they come from far, and a line that is first touched on the way
+// holds everything up.
+__device__ __forceinline__ void touch_arguments(const TreeParams& p) {
+  asm volatile("" ::"s"(p.q), "s"(p.tree), "s"(p.slopes), "s"(p.unit), "s"(p.S), "s"(p.per_unit), "s"(p.scale));
+}
+__device__ __forceinline__ int wave_total(int x) { return lane_of((int)wave_prefix_sum((unsigned)x), 63); }
+__device__ __forceinline__ int tiles_of_keys(const TreeParams& p, int n_keys) {
+  return (n_keys + kTile - 1) / kTile + (p.kt ? (p.T + kTile - 1) / kTile : 0);
+}
 __device__ __forceinline__ int keys_of_unit(const TreeParams& p, int unit) {
   if (p.unit) return p.unit[unit].y;
   return p.n_keys ? min(max(p.n_keys[unit / p.Hkv], 0), p.rows) : p.rows;
 }
-__device__ __forceinline__ int tiles_of_unit(const TreeParams& p, int unit) {
-  return (keys_of_unit(p, unit) + kTile - 1) / kTile + (p.kt ? (p.T + kTile - 1) / kTile : 0);
-}
-// All units of a dense cache have as many.
-__device__ __forceinline__ bool same_units(const TreeParams& p) { return !p.unit && !p.n_keys; }
-__device__ __forceinline__ int shares_used(const TreeParams& p, long long tiles) {
-  const long long most = (tiles + p.min_tiles - 1) / p.min_tiles;
-  return (int)(most < 1 ? 1 : most < p.shares ? most : p.shares);
+
+// A unit's list as it is: lane j has run j of it.  Ids outside the index and ids that were there before are empty runs.
+__device__ __forceinline__ int take_list(const TreeParams& p, int unit, Cursor& c) {
+  const int lane = threadIdx.x & 63, n = p.nprobe + (p.resident >= 0 ? 1 : 0);
+  int b = lane < p.nprobe ? p.selected[(size_t)unit * p.nprobe + lane] : lane < n ? p.resident : -1;
+  // an id that was there before: the later lanes' loses
+  unsigned long long again = 0ull;
+#pragma unroll 4
+  for (int j = 0; j < n; ++j) again |= __ballot(lane_of(b, j) == b) & (~1ull << j);
+  const bool there = (unsigned)b < (unsigned)p.runs && !(again >> lane & 1ull);
+  const int at = there ? b : 0;
+  const int first = min(max(p.off[(size_t)unit * (p.runs + 1) + at], 0), p.rows - 1);
+  const int len = there ? min(max(p.len[(size_t)unit * p.runs + at], 0), p.rows - first) : 0;
+  const int end = (int)wave_prefix_sum((unsigned)len);
+  c.e = make_int4(end - len, first, -1, -1);
+  c.j = c.j0 = 0;
+  return lane_of(end, 63);
 }
 
-// A workgroup's part of the line.
+// A workgroup's share of the tiles: those of one unit.
 struct Share {
-  int lo, hi, unit;                   // tiles [lo, hi); the unit that holds the first
+  int unit, lo, hi;                   // tiles [lo, hi) of its keys and drafted keys
+  int slot, of;                       // place of its partial results; shares of the unit
+  int n_runs, n_keys;
   bool there;
 };
-__device__ __forceinline__ Share find_share(const TreeParams& p, int* s_start /* units + 1 */, int* s_sum, int n_waves) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, threads = 64 * n_waves;
+// Shares of about as many tiles each, as many as the device holds at a time.  No share has tiles of two units: a second unit
+// costs a workgroup its whole way to the first tile again.
+__device__ __forceinline__ Share find_share(const TreeParams& p, Cursor& c) {
+  const int lane = threadIdx.x & 63;
   Share r;
-  int tiles;
-  if (same_units(p)) {
-    const int one = tiles_of_unit(p, 0);
-    tiles = one * p.units;
-    const int used = shares_used(p, tiles);
-    r.there = (int)blockIdx.x < used;
-    r.lo = (int)((long long)tiles * blockIdx.x / used);
-    r.hi = (int)((long long)tiles * (blockIdx.x + 1) / used);
-    r.unit = r.lo / one;
+  int index = 0;
+  if (p.per_unit > 0) {
+    r.unit = __builtin_amdgcn_readfirstlane((int)blockIdx.x / p.per_unit);
+    index = (int)blockIdx.x - r.unit * p.per_unit;
+    r.n_runs = p.nprobe + (p.resident >= 0 ? 1 : 0);
+    r.n_keys = p.listed ? take_list(p, r.unit, c) : p.rows;
+    r.of = min(p.per_unit, max((tiles_of_keys(p, r.n_keys) + p.min_tiles - 1) / p.min_tiles, 1));
+    if (index == 0 && blockIdx.y == 0 && threadIdx.x == 0) p.start[r.unit] = make_int2(r.unit * p.per_unit, r.of);
+    r.there = index < r.of;
   } else {
-    const int per = (p.units + threads - 1) / threads, u0 = min(tid * per, p.units), u1 = min(u0 + per, p.units);
-    int mine = 0;
-    for (int u = u0; u < u1; ++u) mine += tiles_of_unit(p, u);
-    int run = (int)wave_prefix_sum((unsigned)mine);
-    if (lane == 63) s_sum[wave] = run;
-    __syncthreads();
-    run -= mine;
-    tiles = 0;
-    for (int w = 0; w < n_waves; ++w) {
-      run += w < wave ? s_sum[w] : 0;
-      tiles += s_sum[w];
+    // f(unit, its tiles) for the units of all lanes
+    auto for_units = [&](auto f) {
+      for (int u0 = 0; u0 < p.units; u0 += 64) {
+        const int u = u0 + lane;
+        f(u, u < p.units ? tiles_of_keys(p, keys_of_unit(p, u)) : 0);
+      }
+    };
+    int total = 0, most = 0;
+    for_units([&](int, int n) {
+      total += wave_total(n);
+      most = max(most, n);
+    });
+    most = (int)wave_max((float)most);                   // < 2^24
+    // the smallest chunk whose shares fit, in a few steps; with one share to a unit they do
+    int chunk = max((total + p.shares - 1) / p.shares, p.min_tiles), shares = 0;
+    for (int step = 0;; ++step) {
+      shares = 0;
+      for_units([&](int u, int n) { shares += wave_total(u < p.units ? max((n + chunk - 1) / chunk, 1) : 0); });
+      if (shares <= max(p.shares, p.units) || chunk >= most) break;
+      chunk = step < 4 ? min(max(chunk + 1, (int)((long long)chunk * shares / p.shares)), most) : most;
     }
-    for (int u = u0; u < u1; ++u) {
-      s_start[u] = run;
-      run += tiles_of_unit(p, u);
-    }
-    if (tid == 0) s_start[p.units] = tiles;
-    __syncthreads();
-    if (blockIdx.x == 0 && blockIdx.y == 0)
-      for (int u = tid; u <= p.units; u += threads) p.start[u] = s_start[u];
-    tiles = __builtin_amdgcn_readfirstlane(tiles);
-    const int used = shares_used(p, tiles);
-    r.there = (int)blockIdx.x < used;
-    r.lo = (int)((long long)tiles * blockIdx.x / used);
-    r.hi = (int)((long long)tiles * (blockIdx.x + 1) / used);
-    r.unit = 0;
-    for (int step = 1 << (31 - __clz(p.units)); step > 0; step >>= 1)      // the last unit that starts at or before lo
-      if (r.unit + step < p.units && s_start[r.unit + step] <= r.lo) r.unit += step;
+    int before = 0;
+    r.unit = -1;
+    for_units([&](int u, int n) {
+      const int mine = u < p.units ? max((n + chunk - 1) / chunk, 1) : 0;
+      const int end = before + (int)wave_prefix_sum((unsigned)mine), first = end - mine;
+      if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 64 && u < p.units) p.start[u] = make_int2(first, mine);
+      const unsigned long long here = __ballot(mine > 0 && first <= (int)blockIdx.x && (int)blockIdx.x < end);
+      if (here) {
+        const int at = __ffsll(here) - 1;
+        r.unit = lane_of(u, at);
+        index = (int)blockIdx.x - lane_of(first, at);
+        r.of = lane_of(mine, at);
+      }
+      before = lane_of(end, 63);
+    });
+    r.there = r.unit >= 0;
+    if (!r.there) return r;
+    const int2 ru = p.unit ? p.unit[r.unit] : make_int2(1, keys_of_unit(p, r.unit));
+    r.n_runs = __builtin_amdgcn_readfirstlane(ru.x);
+    r.n_keys = __builtin_amdgcn_readfirstlane(ru.y);
   }
-  r.there = r.there && r.lo < r.hi;
-  r.unit = __builtin_amdgcn_readfirstlane(r.unit);
+  const int tiles = tiles_of_keys(p, r.n_keys);
+  r.lo = (int)((long long)tiles * index / r.of);
+  r.hi = (int)((long long)tiles * (index + 1) / r.of);
+  r.slot = blockIdx.x;
   return r;
-}
-__device__ __forceinline__ int first_tile(const TreeParams& p, const int* s_start, int unit) {
-  return same_units(p) ? unit * tiles_of_unit(p, 0) : __builtin_amdgcn_readfirstlane(s_start[unit]);
 }
 
 // What a wave needs of a unit; its rows' queries.
-template <typename C, bool LISTS, bool SHAPED, typename Op>
-__device__ __forceinline__ void enter(const TreeParams& p, int unit, int t, int g, int half, Unit& u, Rows& w, Op& op) {
+template <typename C, bool SHAPED, typename Op>
+__device__ __forceinline__ void enter(const TreeParams& p, const Share& mine, int t, int g, int half, Unit& u, Rows& w, Op& op) {
   typedef typename Op::Query Q;
-  const int s = unit / p.Hkv, h = unit - s * p.Hkv, hq = h * p.G + g;
+  const int unit = mine.unit, s = unit / p.Hkv, h = unit - s * p.Hkv, hq = h * p.G + g;
   const size_t rows_at = (size_t)unit * p.rows, token = (size_t)s * p.T + t;
   op.load_q(static_cast<const Q*>(p.q) + (token * p.Hq + hq) * kD, half);
   u.sees = p.kt ? (unsigned long long)p.tree[token] : 0ull;
@@ -689,9 +731,8 @@ __device__ __forceinline__ void enter(const TreeParams& p, int unit, int t, int 
   u.table = p.table + (size_t)unit * p.cap;
   u.idx = p.idx + rows_at;
   u.pos = p.pos + (size_t)s * p.T;
-  const int2 ru = LISTS ? p.unit[unit] : make_int2(1, 0);
-  u.n_runs = __builtin_amdgcn_readfirstlane(ru.x);
-  u.n_keys = __builtin_amdgcn_readfirstlane(LISTS ? ru.y : keys_of_unit(p, unit));
+  u.n_runs = mine.n_runs;
+  u.n_keys = mine.n_keys;
   u.key_tiles = (u.n_keys + kTile - 1) / kTile;
   u.n_drafted = p.T;
   u.scale = p.scale * (p.kscale ? p.kscale[unit] : 1.f);
@@ -701,6 +742,31 @@ __device__ __forceinline__ void enter(const TreeParams& p, int unit, int t, int 
   w.slope2 = SHAPED && p.slopes ? p.slopes[hq] * kLog2e : 0.f;
   w.at_pos = SHAPED && p.slopes ? u.pos[t] : 0;
   w.cap2 = p.softcap * kLog2e;
+}
+
+// Partial results that another workgroup of the launch reads go past the writer's second cache, and are read past the reader's.
+__device__ __forceinline__ void put_far(void* to, unsigned long long v) {
+  __hip_atomic_store(static_cast<unsigned long long*>(to), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long get_far(const void* from) {
+  return __hip_atomic_load(static_cast<const unsigned long long*>(from), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long pair(float a, float b) {
+  return (unsigned long long)__float_as_uint(b) << 32 | __float_as_uint(a);
+}
+__device__ __forceinline__ float low(unsigned long long x) { return __uint_as_float((unsigned)x); }
+__device__ __forceinline__ float high(unsigned long long x) { return __uint_as_float((unsigned)(x >> 32)); }
+__device__ __forceinline__ void put_row(const TreeParams& p, float* to, const float4& o) {
+  if (p.merged) {
+    put_far(to, pair(o.x, o.y));
+    put_far(to + 2, pair(o.z, o.w));
+  } else {
+    *reinterpret_cast<float4*>(to) = o;
+  }
+}
+__device__ __forceinline__ void put_sum(const TreeParams& p, float2* to, float m, float l) {
+  if (p.merged) put_far(to, pair(m, l));
+  else *to = make_float2(m, l);
 }
 
 // The outputs of a wave's rows go to the partial results of a share; KW waves that walked different tiles for the same rows add
@@ -715,12 +781,12 @@ __device__ __forceinline__ void put_partial(const TreeParams& p, const Rows& w, 
   float l = w.l + other_half(w.l);
   l = marked ? -l : l;
   if (KW == 1) {
-    if (half == 0 && col < left) p.part_ml[slot + col] = make_float2(w.m, l);
+    if (half == 0 && col < left) put_sum(p, p.part_ml + slot + col, w.m, l);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int at = row_of(r, half);
       if (at < left)
-        *reinterpret_cast<float4*>(p.part_o + (slot + at) * kD + 4 * col) = make_float4(w.o[0][r], w.o[1][r], w.o[2][r], w.o[3][r]);
+        put_row(p, p.part_o + (slot + at) * kD + 4 * col, make_float4(w.o[0][r], w.o[1][r], w.o[2][r], w.o[3][r]));
     }
     return;
   }
@@ -744,7 +810,7 @@ __device__ __forceinline__ void put_partial(const TreeParams& p, const Rows& w, 
     L = fmaf(f[k], fabsf(ml[k].y), L);
     any |= k < KW ? __float_as_uint(ml[k].y) : 0u;
   }
-  if (kp == 0 && half == 0 && col < left) p.part_ml[slot + col] = make_float2(M, any >> 31 ? -L : L);
+  if (kp == 0 && half == 0 && col < left) put_sum(p, p.part_ml + slot + col, M, any >> 31 ? -L : L);
   for (int r = kp; r < 16 && row_of(r, 0) < left; r += KW) {
     const int at = row_of(r, half);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -755,7 +821,7 @@ __device__ __forceinline__ void put_partial(const TreeParams& p, const Rows& w, 
       const float4 v = s_o[(k * RW + rw) * kOut + r * 64 + lane];
       o.x = fmaf(fk, v.x, o.x); o.y = fmaf(fk, v.y, o.y); o.z = fmaf(fk, v.z, o.z); o.w = fmaf(fk, v.w, o.w);
     }
-    if (at < left) *reinterpret_cast<float4*>(p.part_o + (slot + at) * kD + 4 * col) = o;
+    if (at < left) put_row(p, p.part_o + (slot + at) * kD + 4 * col, o);
   }
   __syncthreads();
 }

@@ -23,10 +23,12 @@ tree_rows_kernel(TreeParams p) {
   static_assert(KW * 2 * TS * kTileBytes >= kWaves * 16 * 64 * (int)sizeof(float4), "both in one place");
   float2* s_ml = reinterpret_cast<float2*>(s_stage + KW * 2 * TS * kTileBytes);      // [wave][32]
   int* s_pos_all = reinterpret_cast<int*>(s_ml + kWaves * kTile);       // [wave][32]
-  int* s_start = s_pos_all + kWaves * kTile;             // [units + 1]
-  __shared__ int s_sum[kWaves], s_again;
+  __shared__ int s_again;
+  touch_arguments(p);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Share mine = find_share(p, s_start, s_sum, kWaves);
+  Cursor begin;
+  begin.j = begin.j0 = 0;
+  const Share mine = find_share(p, begin);
   if (!mine.there) return;
   const int rw = wave % RW, kp = wave / RW;
   const int row0 = (blockIdx.y * RW + rw) * kTile, row = min(row0 + (lane & 31), p.R - 1), left = p.R - row0;
@@ -35,118 +37,111 @@ tree_rows_kernel(TreeParams p) {
   int* s_pos = s_pos_all + wave * kTile;
   Op op;
   Rows w;
-  int lo = mine.lo;
-  for (int unit = mine.unit; lo < mine.hi; ++unit) {
-    const int first = first_tile(p, s_start, unit), seg_end = min(mine.hi, first_tile(p, s_start, unit + 1));
-    if (seg_end <= lo) continue;                         // a unit without tiles
-    const int n = seg_end - lo, t0 = lo - first + n * kp / KW, t1 = lo - first + n * (kp + 1) / KW;
-    const int stages = ((n + KW - 1) / KW + TS - 1) / TS;          // of the group with the most tiles
-    Unit u;
-    enter<C, LISTS, SHAPED>(p, unit, token, g, lane >> 5, u, w, op);
-    for (bool careful = false;; careful = true) {
-      if (tid == 0) s_again = 0;
-      w.clear();
-      Cursor ahead, c;
-      ahead.j = ahead.j0 = 0;
-      if (LISTS && t0 < min(t1, u.key_tiles)) ahead.find(u, t0 * kTile);
-      c = ahead;
-      u32x4_t piece[TS * kPer];
-      auto fetch = [&](int at_stage) {
+  Unit u;
+  enter<C, SHAPED>(p, mine, token, g, lane >> 5, u, w, op);
+  const int n = mine.hi - mine.lo, t0 = mine.lo + n * kp / KW, t1 = mine.lo + n * (kp + 1) / KW;
+  const int stages = ((n + KW - 1) / KW + TS - 1) / TS;  // of the group with the most tiles
+  for (bool careful = false;; careful = true) {
+    if (tid == 0) s_again = 0;
+    w.clear();
+    Cursor ahead = begin;
+    if (LISTS && t0 < min(t1, u.key_tiles)) ahead.find(p, u, t0 * kTile);
+    Cursor c = ahead;
+    u32x4_t piece[TS * kPer];
+    auto fetch = [&](int at_stage) {
 #pragma unroll
-        for (int j = 0; j < TS; ++j) {
-          const int t = t0 + at_stage * TS + j;
-          if (t >= t1) continue;
+      for (int j = 0; j < TS; ++j) {
+        const int t = t0 + at_stage * TS + j;
+        if (t >= t1) continue;
+        const Place at = locate<LISTS, SHAPED>(p, u, w, ahead, t);
+        if (Op::kCodes && at.drafted) continue;        // twice as long as rows of codes: not fetched ahead
+        const int ln = this_lane();
+        unsigned row[kPer];
+        rows_of_keys<LISTS>(at, row, [&](int m) { return Op::key_of(((m * RW + rw) * 64 + ln) & (kSlots - 1), false); });
+#pragma unroll
+        for (int m = 0; m < kPer; ++m) {
+          const bool values = (m * RW + rw) * 64 >= kSlots;
+          const int slot = ((m * RW + rw) * 64 + ln) & (kSlots - 1);
+          const global_t base = at.drafted ? values ? uniform(u.vt) : uniform(u.kt) : values ? uniform(u.V) : uniform(u.K);
+          piece[j * kPer + m] = stream_from<u32x4_t>(base + (row[m] * Op::row_bytes(false) + Op::piece_of(slot, false)));
+        }
+      }
+    };
+    auto put = [&](int at_stage) {
+      char* to = stage + (at_stage & 1) * (TS * kTileBytes);
+      const int ln = this_lane();
+#pragma unroll
+      for (int j = 0; j < TS; ++j) {
+        const int t = t0 + at_stage * TS + j;
+        if (t >= t1) continue;
+        if (Op::kCodes && t >= u.key_tiles) {
           const Place at = locate<LISTS, SHAPED>(p, u, w, ahead, t);
-          if (Op::kCodes && at.drafted) continue;        // twice as long as rows of codes: not fetched ahead
-          const int ln = this_lane();
-          unsigned row[kPer];
-          rows_of_keys<LISTS>(at, row, [&](int m) { return Op::key_of(((m * RW + rw) * 64 + ln) & (kSlots - 1), false); });
+#pragma unroll 1
+          for (int m = 0; m < 1024 / (64 * RW); ++m) {
+            const int all = (m * RW + rw) * 64 + ln, slot = all & 511;
+            const global_t base = (m * RW + rw) * 64 >= 512 ? uniform(u.vt) : uniform(u.kt);
+            const unsigned row = (unsigned)row_of_key<false>(at, Op::key_of(slot, true));
+            *reinterpret_cast<u32x4_t*>(to + j * kTileBytes + Op::key_of(all, true) * Op::stage_row(true) + Op::piece_of(slot, true)) =
+                stream_from<u32x4_t>(base + (row * Op::row_bytes(true) + Op::piece_of(slot, true)));
+          }
+        } else {
 #pragma unroll
           for (int m = 0; m < kPer; ++m) {
-            const bool values = (m * RW + rw) * 64 >= kSlots;
-            const int slot = ((m * RW + rw) * 64 + ln) & (kSlots - 1);
-            const global_t base = at.drafted ? values ? uniform(u.vt) : uniform(u.kt) : values ? uniform(u.V) : uniform(u.K);
-            piece[j * kPer + m] = stream_from<u32x4_t>(base + (row[m] * Op::row_bytes(false) + Op::piece_of(slot, false)));
+            const int slot = (m * RW + rw) * 64 + ln;  // keys, then values
+            *reinterpret_cast<u32x4_t*>(to + j * kTileBytes + Op::key_of(slot, false) * Op::stage_row(false) + Op::piece_of(slot, false)) =
+                piece[j * kPer + m];
           }
         }
-      };
-      auto put = [&](int at_stage) {
-        char* to = stage + (at_stage & 1) * (TS * kTileBytes);
-        const int ln = this_lane();
-#pragma unroll
-        for (int j = 0; j < TS; ++j) {
-          const int t = t0 + at_stage * TS + j;
-          if (t >= t1) continue;
-          if (Op::kCodes && t >= u.key_tiles) {
-            const Place at = locate<LISTS, SHAPED>(p, u, w, ahead, t);
-#pragma unroll 1
-            for (int m = 0; m < 1024 / (64 * RW); ++m) {
-              const int all = (m * RW + rw) * 64 + ln, slot = all & 511;
-              const global_t base = (m * RW + rw) * 64 >= 512 ? uniform(u.vt) : uniform(u.kt);
-              const unsigned row = (unsigned)row_of_key<false>(at, Op::key_of(slot, true));
-              *reinterpret_cast<u32x4_t*>(to + j * kTileBytes + Op::key_of(all, true) * Op::stage_row(true) + Op::piece_of(slot, true)) =
-                  stream_from<u32x4_t>(base + (row * Op::row_bytes(true) + Op::piece_of(slot, true)));
-            }
-          } else {
-#pragma unroll
-            for (int m = 0; m < kPer; ++m) {
-              const int slot = (m * RW + rw) * 64 + ln;  // keys, then values
-              *reinterpret_cast<u32x4_t*>(to + j * kTileBytes + Op::key_of(slot, false) * Op::stage_row(false) + Op::piece_of(slot, false)) =
-                  piece[j * kPer + m];
-            }
-          }
-        }
-      };
-      Place next;
-      if (t0 < t1) next = locate<LISTS, SHAPED>(p, u, w, c, t0);
-      fetch(0);
-      put(0);
-      fetch(1);
-      __syncthreads();
-#pragma unroll 1
-      for (int i = 0; i < stages; ++i) {
-#pragma unroll 1
-        for (int j = 0; j < TS; ++j) {
-          const int t = t0 + i * TS + j;
-          if (t >= t1) break;
-          const Place at = next;
-          if (t + 1 < t1) next = locate<LISTS, SHAPED>(p, u, w, c, t + 1);
-          if (__ballot(at.word != 0u) == 0ull) continue; // none of the wave's rows attends it
-          const char* tile = stage + ((i & 1) * TS + j) * kTileBytes;
-          const int ln = this_lane(), col = ln & 31, half = ln >> 5;
-          f32x16_t s = op.scores(tile, col, half, at.drafted);
-          const unsigned attended = weigh<SHAPED>(p, u, w, at, s, s_pos, col, half);
-          if (u.vscale != 1.f && !at.drafted)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] *= u.vscale;
-          op.stage_v(tile + kTile * Op::stage_row(at.drafted), col, half, at.drafted);
-          op.widen_v(at.drafted);
-          if (careful || at.drafted) w.marked |= op.zero_no_numbers() & attended;
-          op.add(w.o, s);
-        }
-        if (i + 1 < stages) {
-          put(i + 1);
-          fetch(i + 2);
-        }
-        __syncthreads();
       }
-      // outputs that are no numbers: all waves walk again, since all bring the tiles
-      if (w.has_no_numbers() && lane == 0) s_again = 1;
+    };
+    Place next;
+    if (t0 < t1) next = locate<LISTS, SHAPED>(p, u, w, c, t0);
+    fetch(0);
+    put(0);
+    fetch(1);
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < stages; ++i) {
+#pragma unroll 1
+      for (int j = 0; j < TS; ++j) {
+        const int t = t0 + i * TS + j;
+        if (t >= t1) break;
+        const Place at = next;
+        if (t + 1 < t1) next = locate<LISTS, SHAPED>(p, u, w, c, t + 1);
+        if (__ballot(at.word != 0u) == 0ull) continue; // none of the wave's rows attends it
+        const char* tile = stage + ((i & 1) * TS + j) * kTileBytes;
+        const int ln = this_lane(), col = ln & 31, half = ln >> 5;
+        f32x16_t s = op.scores(tile, col, half, at.drafted);
+        const unsigned attended = weigh<SHAPED>(p, u, w, at, s, s_pos, col, half);
+        if (u.vscale != 1.f && !at.drafted)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] *= u.vscale;
+        op.stage_v(tile + kTile * Op::stage_row(at.drafted), col, half, at.drafted);
+        op.widen_v(at.drafted);
+        if (careful || at.drafted) w.marked |= op.zero_no_numbers() & attended;
+        op.add(w.o, s);
+      }
+      if (i + 1 < stages) {
+        put(i + 1);
+        fetch(i + 2);
+      }
       __syncthreads();
-      const bool again = s_again != 0;
-      __syncthreads();
-      if (careful || !again) break;
     }
-    put_partial<kWaves, 16 * 64>(p, w, ((size_t)blockIdx.x + unit) * p.R + row0, left, RW, wave, reinterpret_cast<float4*>(s_stage), s_ml);
-    lo = seg_end;
+    // outputs that are no numbers: all waves walk again, since all bring the tiles
+    if (w.has_no_numbers() && lane == 0) s_again = 1;
+    __syncthreads();
+    const bool again = s_again != 0;
+    __syncthreads();
+    if (careful || !again) break;
   }
+  put_partial<kWaves, 16 * 64>(p, w, (size_t)mine.slot * p.R + row0, left, RW, wave, reinterpret_cast<float4*>(s_stage), s_ml);
 }
 
 template <typename C, bool LISTS, bool SHAPED, int PARTS, int RW>
 bool launch(const TreeParams& p, int blocks, hipStream_t hs) {
-  const size_t lds = (size_t)8 * kTileBytes + sizeof(float2) * kWaves * kTile + sizeof(int) * (kWaves * kTile + p.units + 1);
+  const size_t lds = (size_t)8 * kTileBytes + sizeof(float2) * kWaves * kTile + sizeof(int) * kWaves * kTile;
   if (!allow_lds<tree_rows_kernel<C, LISTS, SHAPED, PARTS, RW>>(lds)) return false;
-  hipLaunchKernelGGL((tree_rows_kernel<C, LISTS, SHAPED, PARTS, RW>), dim3((unsigned)p.shares, (unsigned)blocks), dim3(64 * kWaves), lds, hs, p);
+  hipLaunchKernelGGL((tree_rows_kernel<C, LISTS, SHAPED, PARTS, RW>), dim3((unsigned)p.grid, (unsigned)blocks), dim3(64 * kWaves), lds, hs, p);
   return true;
 }
 template <typename C, bool LISTS, bool SHAPED, int PARTS>
