@@ -55,55 +55,53 @@ __device__ __forceinline__ void angles(const RotateParams& p, long long token0, 
   __builtin_amdgcn_wave_barrier();
 }
 
-// The (cos, sin) of a lane's eight features: pair e of them in c[e], s[e] (pairs: feature 2i and 2i+1 share one).
-__device__ __forceinline__ void read_angles(const RotateParams& p, const float2* cs, int sub, float (&c)[8], float (&s)[8]) {
-  if (p.pairs) {
+// The (cos, sin) of a lane's eight features (PAIRS: feature 2i and 2i+1 share one).
+template <bool PAIRS>
+struct Angles {
+  static constexpr int kOwn = PAIRS ? 4 : 8;
+  float c[kOwn], s[kOwn];
+  __device__ __forceinline__ void read(const RotateParams& p, const float2* cs, int sub) {
+    const int m = p.rot / 16, first = PAIRS ? sub * 4 : (sub < m ? sub : sub - m) * 8;
+    const float4* from = reinterpret_cast<const float4*>(cs + (first & 63));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 v = cs[(sub * 4 + i) & 63];
-      c[2 * i] = c[2 * i + 1] = v.x;
-      s[2 * i] = s[2 * i + 1] = v.y;
-    }
-  } else {
-    const int m = p.rot / 16, first = (sub < m ? sub : sub - m) * 8;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 v = cs[(first + i) & 63];
+    for (int i = 0; i < kOwn; i += 2) {
+      const float4 v = from[i / 2];
       c[i] = v.x;
       s[i] = v.y;
+      c[i + 1] = v.z;
+      s[i + 1] = v.w;
     }
   }
-}
+};
 
 // y turned by the angles (forward), or turned back (BACK): rows of 16 lanes.
-template <bool BACK>
-__device__ __forceinline__ void turn(const RotateParams& p, int sub, const float (&c)[8], const float (&s)[8], const float (&y)[8],
-                                     float (&out)[8]) {
-  if (p.pairs) {
+template <bool BACK, bool PAIRS>
+__device__ __forceinline__ void turn(const RotateParams& p, int sub, const Angles<PAIRS>& at, float (&y)[8]) {
+  if constexpr (PAIRS) {
     const bool in = sub * 8 < p.rot;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) {
-      const float sn = BACK ? -s[i] : s[i];
-      out[i] = in ? y[i] * c[i] - y[i + 1] * sn : y[i];
-      out[i + 1] = in ? y[i + 1] * c[i] + y[i] * sn : y[i + 1];
+    for (int i = 0; i < 4; ++i) {
+      const float a = y[2 * i], b = y[2 * i + 1], sn = BACK ? -at.s[i] : at.s[i];
+      y[2 * i] = in ? a * at.c[i] - b * sn : a;
+      y[2 * i + 1] = in ? b * at.c[i] + a * sn : b;
     }
-    return;
-  }
-  const int m = p.rot / 16;                              // lanes of half of the turned features
-  const bool first = sub < m, in = sub < 2 * m;
-  float other[8];
-  if (m == 8) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) other[i] = dpp_mov<0x128 /* row_ror:8 */>(y[i]);
   } else {
-    const int from = (threadIdx.x & 48) + (first ? sub + m : in ? sub - m : sub);
+    const int m = p.rot / 16;                            // lanes of half of the turned features
+    const bool first = sub < m, in = sub < 2 * m;
+    float other[8];
+    if (m == 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) other[i] = __shfl(y[i], from);
-  }
+      for (int i = 0; i < 8; ++i) other[i] = dpp_mov<0x128 /* row_ror:8 */>(y[i]);
+    } else {
+      const int from = (threadIdx.x & 48) + (first ? sub + m : in ? sub - m : sub);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float sn = first != BACK ? -s[i] : s[i];       // a cos - b sin, b cos + a sin; turned back with the other sign
-    out[i] = in ? y[i] * c[i] + other[i] * sn : y[i];
+      for (int i = 0; i < 8; ++i) other[i] = __shfl(y[i], from);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float sn = first != BACK ? -at.s[i] : at.s[i];         // a cos - b sin, b cos + a sin; turned back with the other sign
+      y[i] = in ? y[i] * at.c[i] + other[i] * sn : y[i];
+    }
   }
 }
 
@@ -121,136 +119,156 @@ __device__ __forceinline__ void load8(const float* from, float (&v)[8]) {
   x.to_float(v);
 }
 
+// A load of what is read once.  A bf16 row is one load of 16 lanes: past the caches (the gradients of 4 x 4096 tokens: 141 us instead
+// of 148).  An fp32 row takes two, each with half of every line: through them (777 tokens of 16 + 16 heads: 12 us, past them 15).
+template <typename T>
+__device__ __forceinline__ void load_once(Vec8<T>& v, const T* from) {
+  if constexpr (sizeof(T) == 2) v.load_stream(from);
+  else v.load(from);
+}
+
 // Where the row of a lane is: quad `quad` of the head line (q's heads, then k's), the wave's lane group `grp`.
+template <int TW>
+struct Place {
+  unsigned token, s, t;               // the lane's token (the last one where there is none), its sequence and place there
+  bool there;
+  __device__ __forceinline__ Place(const RotateParams& p, long long token0, int grp) {
+    const long long at = token0 + grp % TW;
+    there = at < p.tokens;
+    token = (unsigned)(there ? at : p.tokens - 1);
+    s = token / (unsigned)p.T;
+    t = token - s * (unsigned)p.T;
+  }
+};
 struct Row {
-  bool is_q, there;
+  bool is_q;
   int head;
-  long long token;
 };
 template <int TW>
-__device__ __forceinline__ Row row_at(const RotateParams& p, long long token0, int quad, int grp) {
+__device__ __forceinline__ Row row_at(const RotateParams& p, int quad, int grp) {
   Row r;
   r.is_q = quad < p.q_quads;
   r.head = (r.is_q ? quad : quad - p.q_quads) * (4 / TW) + grp / TW;
-  r.token = token0 + grp % TW;
-  r.there = r.token < p.tokens;
   return r;
 }
-// Offset of a row in a tensor of k's layout [S,Hkv,T,d].
-__device__ __forceinline__ size_t heads_first(const RotateParams& p, const Row& r) {
-  const long long s = r.token / p.T;
-  return ((size_t)(s * p.Hkv + r.head) * p.T + (size_t)(r.token - s * p.T)) * kD;
+// Offset of a row in tensors of q's layout [S,T,Hq,d], k's layout [S,Hkv,T,d].
+template <int TW>
+__device__ __forceinline__ size_t offset_of(const RotateParams& p, const Place<TW>& at, const Row& r) {
+  return (r.is_q ? (size_t)at.token * p.Hq + r.head : ((size_t)at.s * p.Hkv + r.head) * p.T + at.t) * kD;
+}
+template <typename T, int TW>
+__device__ __forceinline__ const T* input_at(const RotateParams& p, const Place<TW>& at, const Row& r) {
+  const T* x = r.is_q ? static_cast<const T*>(p.q) + (size_t)at.token * p.q_stride : static_cast<const T*>(p.k) + (size_t)at.token * p.k_stride;
+  return x + r.head * kD;
+}
+// 1 / sqrt(mean(x^2) + eps) of a row of 16 lanes.
+__device__ __forceinline__ float scale_of(const RotateParams& p, const float (&x)[8]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
+  return rsqrtf(sum16(sum) * (1.0f / kD) + p.eps);
+}
+__device__ __forceinline__ void load_weight(const RotateParams& p, const Row& r, int sub, float (&w)[8]) {
+  const float* from = r.is_q ? p.q_weight : p.k_weight;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = 1.f;
+  if (from) load8(from + (p.per_head ? r.head * kD : 0) + sub * 8, w);
 }
 
 // A wave: TW tokens, `chunk` quads of heads.
-template <typename T, int TW>
+template <typename T, int TW, bool PAIRS>
 __global__ void __launch_bounds__(64 * kWaves)
 norm_rotate_kernel(RotateParams p) {
-  __shared__ float2 s_cs[kWaves][TW * 64];
+  __shared__ __align__(16) float2 s_cs[kWaves][TW * 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane & 15, grp = lane >> 4;
-  const long long groups = (p.tokens + TW - 1) / TW;
-  const int chunks = (p.quads + p.chunk - 1) / p.chunk;
-  const long long at = (long long)blockIdx.x * kWaves + wave;
-  const long long group = at / chunks;
-  const int quad0 = (int)(at - group * chunks) * p.chunk, quad1 = min(quad0 + p.chunk, p.quads);
+  const unsigned groups = (unsigned)((p.tokens + TW - 1) / TW), chunks = (unsigned)(p.quads + p.chunk - 1) / (unsigned)p.chunk;
+  const unsigned long long at_all = (unsigned long long)blockIdx.x * kWaves + wave;
+  const unsigned group = (unsigned)(at_all / chunks);
+  const int quad0 = (int)(at_all - (unsigned long long)group * chunks) * p.chunk, quad1 = min(quad0 + p.chunk, p.quads);
   if (group >= groups) return;
-  const long long token0 = group * TW;
-  auto fetch = [&](int quad, Vec8<T>& x) {
-    const Row r = row_at<TW>(p, token0, quad, grp);
-    const long long token = r.there ? r.token : p.tokens - 1;
-    const T* from = r.is_q ? static_cast<const T*>(p.q) + token * p.q_stride : static_cast<const T*>(p.k) + token * p.k_stride;
-    x.load(from + r.head * kD + sub * 8);
-  };
+  const long long token0 = (long long)group * TW;
+  const Place<TW> at(p, token0, grp);
   Vec8<T> x;
-  fetch(quad0, x);
+  x.load(input_at<T>(p, at, row_at<TW>(p, quad0, grp)) + sub * 8);
   angles<TW>(p, token0, s_cs[wave]);
-  float c[8], s[8];
-  read_angles(p, s_cs[wave] + (grp % TW) * 64, sub, c, s);
+  Angles<PAIRS> cs;
+  cs.read(p, s_cs[wave] + (grp % TW) * 64, sub);
   for (int quad = quad0; quad < quad1; ++quad) {
-    const Row r = row_at<TW>(p, token0, quad, grp);
-    float y[8], t[8];
+    const Row r = row_at<TW>(p, quad, grp);
+    float y[8];
     x.to_float(y);
-    if (quad + 1 < quad1) fetch(quad + 1, x);
+    if (quad + 1 < quad1) x.load(input_at<T>(p, at, row_at<TW>(p, quad + 1, grp)) + sub * 8);
     if (p.norm) {
-      float sum = 0.f;
+      float w[8];
+      load_weight(p, r, sub, w);
+      const float inv = scale_of(p, y);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(y[i], y[i], sum);
-      const float inv = 1.0f / sqrtf(sum16(sum) * (1.0f / kD) + p.eps);
-      const float* w = r.is_q ? p.q_weight : p.k_weight;
-      float wv[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-      if (w) load8(w + (p.per_head ? r.head * kD : 0) + sub * 8, wv);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = y[i] * inv * wv[i];
+      for (int i = 0; i < 8; ++i) y[i] = y[i] * inv * w[i];
     }
-    turn<false>(p, sub, c, s, y, t);
-    if (!r.there) continue;
-    const size_t to = r.is_q ? ((size_t)r.token * p.Hq + r.head) * kD : heads_first(p, r);
+    const size_t to = offset_of(p, at, r) + sub * 8;
     T* feat = static_cast<T*>(r.is_q ? p.q_feat : p.k_feat);
     T* rotated = static_cast<T*>(r.is_q ? p.q_rot : p.k_rot);
-    if (feat) store8<T>(feat + to + sub * 8, y);
-    if (rotated) store8<T>(rotated + to + sub * 8, t);
+    if (feat && at.there) store8<T>(feat + to, y);
+    turn<false>(p, sub, cs, y);
+    if (rotated && at.there) store8<T>(rotated + to, y);
   }
 }
 
-// A workgroup: one quad of heads, `chunk` groups of TW tokens, dealt to its waves in turn.
-template <typename T, int TW>
+// A workgroup: one quad of heads, `chunk` groups of TW tokens, dealt to its waves in turn.  The next group's rows are on their way
+// while one is worked on.
+template <typename T, int TW, bool PAIRS>
 __global__ void __launch_bounds__(64 * kWaves)
 norm_rotate_grads_kernel(RotateParams p) {
-  __shared__ float2 s_cs[kWaves][TW * 64];
+  __shared__ __align__(16) float2 s_cs[kWaves][TW * 64];
   __shared__ float4 s_dw[kWaves][64][2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane & 15, grp = lane >> 4;
   const int quad = blockIdx.y;
+  const Row r = row_at<TW>(p, quad, grp);
   const long long groups = (p.tokens + TW - 1) / TW, g0 = (long long)blockIdx.x * p.chunk, g1 = min(g0 + p.chunk, groups);
-  float dw[8] = {0.f};
+  const T* feat = static_cast<const T*>(r.is_q ? p.q_feat : p.k_feat);
+  const T* rotated = static_cast<const T*>(r.is_q ? p.q_rot : p.k_rot);
+  T* to = static_cast<T*>(r.is_q ? p.dq : p.dk);
+  const int heads = r.is_q ? p.Hq : p.Hkv;
+  float dw[8] = {0.f}, w[8];
+  load_weight(p, r, sub, w);
+  Vec8<T> vx, vf, vr;
+  auto fetch = [&](const Place<TW>& at) {
+    const size_t from = offset_of(p, at, r) + sub * 8;
+    load_once(vx, input_at<T>(p, at, r) + sub * 8);
+    if (rotated) load_once(vr, rotated + from);
+    if (feat) load_once(vf, feat + from);
+  };
+  if (g0 + wave < g1) fetch(Place<TW>(p, (g0 + wave) * TW, grp));
   for (long long group = g0 + wave; group < g1; group += kWaves) {
-    const long long token0 = group * TW;
-    Row r = row_at<TW>(p, token0, quad, grp);
-    const bool there = r.there;
-    if (!there) r.token = p.tokens - 1;
-    const T* from = r.is_q ? static_cast<const T*>(p.q) + r.token * p.q_stride : static_cast<const T*>(p.k) + r.token * p.k_stride;
-    const size_t at = r.is_q ? ((size_t)r.token * p.Hq + r.head) * kD : heads_first(p, r);
-    const T* feat = static_cast<const T*>(r.is_q ? p.q_feat : p.k_feat);
-    const T* rotated = static_cast<const T*>(r.is_q ? p.q_rot : p.k_rot);
-    Vec8<T> vx, vf, vr;
-    vx.load(from + r.head * kD + sub * 8);
-    if (rotated) vr.load(rotated + at + sub * 8);
-    if (feat) vf.load(feat + at + sub * 8);
-    float g[8] = {0.f};
+    const Place<TW> at(p, group * TW, grp);
+    float g[8], f[8], x[8];
+    vr.to_float(g);
+    vf.to_float(f);
+    vx.to_float(x);
+    if (group + kWaves < g1) fetch(Place<TW>(p, (group + kWaves) * TW, grp));
     if (rotated) {
-      float c[8], s[8], t[8];
-      angles<TW>(p, token0, s_cs[wave]);
-      read_angles(p, s_cs[wave] + (grp % TW) * 64, sub, c, s);
-      vr.to_float(t);
-      turn<true>(p, sub, c, s, t, g);
+      Angles<PAIRS> cs;
+      angles<TW>(p, group * TW, s_cs[wave]);
+      cs.read(p, s_cs[wave] + (grp % TW) * 64, sub);
+      turn<true>(p, sub, cs, g);
     }
-    if (feat) {
-      float f[8];
-      vf.to_float(f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] += f[i];
-    }
+    for (int i = 0; i < 8; ++i) g[i] = (rotated ? g[i] : 0.f) + (feat ? f[i] : 0.f);
     if (p.norm) {
-      float x[8], sum = 0.f, dot = 0.f;
-      vx.to_float(x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-      const float inv = 1.0f / sqrtf(sum16(sum) * (1.0f / kD) + p.eps);
-      const float* w = r.is_q ? p.q_weight : p.k_weight;
-      float wv[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-      if (w) load8(w + (p.per_head ? r.head * kD : 0) + sub * 8, wv);
+      const float inv = scale_of(p, x);
+      float dot = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         x[i] *= inv;
-        dw[i] = there ? fmaf(g[i], x[i], dw[i]) : dw[i];
-        g[i] *= wv[i];
+        dw[i] = at.there ? fmaf(g[i], x[i], dw[i]) : dw[i];
+        g[i] *= w[i];
         dot = fmaf(g[i], x[i], dot);
       }
       dot = sum16(dot) * (1.0f / kD);
 #pragma unroll
       for (int i = 0; i < 8; ++i) g[i] = inv * (g[i] - x[i] * dot);
     }
-    T* to = static_cast<T*>(r.is_q ? p.dq : p.dk);
-    if (there && to) store8<T>(to + ((size_t)r.token * (r.is_q ? p.Hq : p.Hkv) + r.head) * kD + sub * 8, g);
+    if (at.there) store8<T>(to + ((size_t)at.token * heads + r.head) * kD + sub * 8, g);
   }
   if (!p.part) return;
   s_dw[wave][lane][0] = make_float4(dw[0], dw[1], dw[2], dw[3]);
@@ -267,9 +285,9 @@ norm_rotate_grads_kernel(RotateParams p) {
       a.x += u.x; a.y += u.y; a.z += u.z; a.w += u.w;
       b.x += v.x; b.y += v.y; b.z += v.z; b.w += v.w;
     }
-  float* to = p.part + (((size_t)blockIdx.x * p.quads + quad) * rows + grp) * kD + sub * 8;
-  *reinterpret_cast<float4*>(to) = a;
-  *reinterpret_cast<float4*>(to + 4) = b;
+  float* part = p.part + (((size_t)blockIdx.x * p.quads + quad) * rows + grp) * kD + sub * 8;
+  *reinterpret_cast<float4*>(part) = a;
+  *reinterpret_cast<float4*>(part + 4) = b;
 }
 
 // The weights' gradients from the workgroups' sums, in a fixed order.  A workgroup: 16 features of one weight row (blockIdx.x:
@@ -287,19 +305,13 @@ weight_grads_kernel(const float* __restrict__ part, float* __restrict__ dq_weigh
   // the weight row's quads, and within a quad its lane groups (shared weights: one sum to a quad)
   const int rows = per_head ? 4 : 1, quad0 = (is_q ? 0 : q_quads) + (per_head ? row * TW / 4 : 0);
   const int n_quads = per_head ? 1 : is_q ? q_quads : quads - q_quads, grp0 = per_head ? row * TW % 4 : 0, n_grp = per_head ? TW : 1;
-  const int n = chunks * n_quads * n_grp;
-  const float* from = part + blockIdx.x * 16 + f;
+  const float* from = part + (size_t)(quad0 * rows + grp0) * kD + blockIdx.x * 16 + f;
+  const size_t stride = (size_t)quads * rows * kD;       // between chunks
+  const int n = n_quads * n_grp;                         // rows of a chunk, one after the other (one of the two is 1)
   float sum = 0.f;
-  for (int i0 = mine; i0 < n; i0 += 8 * kSumParts) {
-    float v[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int i = min(i0 + u * kSumParts, n - 1), g = i % n_grp, j = i / n_grp, quad = quad0 + j % n_quads, chunk = j / n_quads;
-      v[u] = from[(((size_t)chunk * quads + quad) * rows + grp0 + g) * kD];
-    }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) sum += i0 + u * kSumParts < n ? v[u] : 0.f;
-  }
+  for (int chunk = mine; chunk < chunks; chunk += kSumParts)
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) sum += from[chunk * stride + i * kD];
   s_sum[mine][f] = sum;
   __syncthreads();
   for (int step = kSumParts / 2; step > 0; step >>= 1) {
@@ -341,14 +353,20 @@ RotateParams params_of(const saap_rotation* a, const void* q, const void* k, int
   return p;
 }
 
-// Backward: a workgroup's share of the tokens.  Eight workgroups to a compute unit over all quads; no fewer than two rounds of
-// a workgroup's waves, so that the sums to be added up stay few.
+// Backward: a workgroup's share of the tokens.  Four workgroups to a compute unit over all quads, which is what their registers
+// leave room for at a time (eight take as long, 148 us for 4 x 4096 tokens, and leave twice the sums to add up: 6.4 us, not 4.9); no
+// fewer than two rounds of a workgroup's waves, so that the sums stay few.
 long long grads_chunk(long long groups, int quads) {
-  const long long wanted = 8LL * device_cus() / quads + 1;
+  const long long wanted = 4LL * device_cus() / quads + 1;
   const long long per = (groups + wanted - 1) / wanted;
   return per < 2 * kWaves ? 2 * kWaves : per;
 }
 
+template <typename T, int TW>
+void launch_rotate(const RotateParams& p, unsigned blocks, hipStream_t hs) {
+  if (p.pairs) hipLaunchKernelGGL((norm_rotate_kernel<T, TW, true>), dim3(blocks), dim3(64 * kWaves), 0, hs, p);
+  else hipLaunchKernelGGL((norm_rotate_kernel<T, TW, false>), dim3(blocks), dim3(64 * kWaves), 0, hs, p);
+}
 template <typename T>
 void launch_rotate(RotateParams& p, int TW, hipStream_t hs) {
   const long long groups = (p.tokens + TW - 1) / TW;
@@ -359,17 +377,22 @@ void launch_rotate(RotateParams& p, int TW, hipStream_t hs) {
   per = per < 1 ? 1 : per > p.quads ? p.quads : per;
   p.chunk = (int)per;
   const long long chunks = (p.quads + per - 1) / per;
-  const dim3 grid((unsigned)((groups * chunks + kWaves - 1) / kWaves)), block(64 * kWaves);
-  if (TW == 1) hipLaunchKernelGGL((norm_rotate_kernel<T, 1>), grid, block, 0, hs, p);
-  else if (TW == 2) hipLaunchKernelGGL((norm_rotate_kernel<T, 2>), grid, block, 0, hs, p);
-  else hipLaunchKernelGGL((norm_rotate_kernel<T, 4>), grid, block, 0, hs, p);
+  const unsigned blocks = (unsigned)((groups * chunks + kWaves - 1) / kWaves);
+  if (TW == 1) launch_rotate<T, 1>(p, blocks, hs);
+  else if (TW == 2) launch_rotate<T, 2>(p, blocks, hs);
+  else launch_rotate<T, 4>(p, blocks, hs);
+}
+template <typename T, int TW>
+void launch_grads(const RotateParams& p, unsigned chunks, hipStream_t hs) {
+  const dim3 grid(chunks, (unsigned)p.quads), block(64 * kWaves);
+  if (p.pairs) hipLaunchKernelGGL((norm_rotate_grads_kernel<T, TW, true>), grid, block, 0, hs, p);
+  else hipLaunchKernelGGL((norm_rotate_grads_kernel<T, TW, false>), grid, block, 0, hs, p);
 }
 template <typename T>
 void launch_grads(const RotateParams& p, int TW, unsigned chunks, hipStream_t hs) {
-  const dim3 grid(chunks, (unsigned)p.quads), block(64 * kWaves);
-  if (TW == 1) hipLaunchKernelGGL((norm_rotate_grads_kernel<T, 1>), grid, block, 0, hs, p);
-  else if (TW == 2) hipLaunchKernelGGL((norm_rotate_grads_kernel<T, 2>), grid, block, 0, hs, p);
-  else hipLaunchKernelGGL((norm_rotate_grads_kernel<T, 4>), grid, block, 0, hs, p);
+  if (TW == 1) launch_grads<T, 1>(p, chunks, hs);
+  else if (TW == 2) launch_grads<T, 2>(p, chunks, hs);
+  else launch_grads<T, 4>(p, chunks, hs);
 }
 
 }  // namespace
