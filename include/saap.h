@@ -853,7 +853,8 @@ int32_t saap_window_push_fp8(const void* x_new, const void* k_new, const void* v
  *   q_feat, q_rot [S,T,Hq,d] dtype, out (token-major, as the decode calls take queries);
  *   k_feat, k_rot [S,Hkv,T,d] dtype, out (head-major, as assign_keys, build_bucket_index and the trees take keys)
  *   Of the two outputs of a given tensor either may be NULL.  Outputs must not overlap inputs.
- * rot is a multiple of 16 up to d.  Sums, angles and products are in fp32 (angles' reduction in fp64), rounded once.
+ * rot is a multiple of 16 up to d; S*T <= 2^25; Hq, Hkv <= 4096.  Sums, angles and products are in fp32 (angles' reduction in
+ * fp64), rounded once.
  */
 typedef struct {
   const int32_t* positions;

@@ -335,7 +335,8 @@ int32_t check(const saap_rotation* a, const void* q, const void* k) {
   if (q && (a->q_stride < (long long)a->Hq * kD || a->q_stride % piece)) return SAAP_INVALID_ARG;
   if (k && (a->k_stride < (long long)a->Hkv * kD || a->k_stride % piece)) return SAAP_INVALID_ARG;
   if (a->d != kD || a->rot > kD || a->rot % 16) return SAAP_UNSUPPORTED;
-  if ((long long)a->S * a->T > 0x7fffffffLL || a->Hq > 4096 || a->Hkv > 4096) return SAAP_UNSUPPORTED;
+  // a launch has fewer than 2^32 threads: 64 to a token at most
+  if ((long long)a->S * a->T > 1LL << 25 || a->Hq > 4096 || a->Hkv > 4096) return SAAP_UNSUPPORTED;
   return SAAP_OK;
 }
 

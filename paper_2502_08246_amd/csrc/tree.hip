@@ -156,8 +156,8 @@ __device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit
     M = mn;
     // a thread to a feature
     if (tid < kD)
+#pragma unroll 4
       for (int i = 0; i < min(256, n - base); ++i) {
-        if (s_w[i] < 0.f) continue;
         const int key_i = base + i;
         float v;
         if (key_i >= n_keys) {
@@ -168,7 +168,7 @@ __device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit
           if (lists) r = row_of_key(key_i, in_list);
           v = element<C>(static_cast<const char*>(p.V) + ((size_t)unit * p.rows + r) * (kD * sizeof(C)), tid) * (p.vscale ? p.vscale[unit] : 1.f);
         }
-        acc = fmaf(s_w[i], v, acc);
+        acc = s_w[i] < 0.f ? acc : fmaf(s_w[i], v, acc);
       }
     __syncthreads();
   }
@@ -448,11 +448,12 @@ int32_t attend(const saap_tree* a, const void* q, const void* K, const void* V, 
   p.lists = lists_per_token ? a->T : 1; p.resident = resident_run; p.cap = at.cap; p.shares = at.shares; p.units = (int)units;
   p.out_bf16 = out_dtype == SAAP_BF16; p.RW = at.RW; p.min_tiles = at.min_tiles; p.scale = a->scale; p.softcap = a->softcap;
   // One list to a unit, short enough for the lanes of a wave: nothing to plan.  Such lists, and dense caches of one length, have
-  // about as many keys each: every unit has as many shares.
+  // about as many keys each: every unit has as many shares.  Where there are as many units as shares, every unit is one: 4096 units
+  // of up to 100 keys 98 us (all workgroups working the shares out from all units' keys: 542), of up to 1000 keys 280 (680).
   p.listed = lists && p.lists == 1 && nprobe + (resident_run >= 0 ? 1 : 0) <= 63;
   p.unit = lists && !p.listed ? reinterpret_cast<int2*>(base + at.unit) : nullptr;
   p.grid = at.grid;
-  if (p.listed || (!lists && !n_keys)) {
+  if (p.listed || (!lists && !n_keys) || units >= at.shares) {
     p.per_unit = at.shares > units ? (int)(at.shares / units) : 1;
     if (!lists) {
       // dense: no more than there are

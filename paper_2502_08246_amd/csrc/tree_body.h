@@ -661,8 +661,8 @@ __device__ __forceinline__ Share find_share(const TreeParams& p, Cursor& c) {
   if (p.per_unit > 0) {
     r.unit = __builtin_amdgcn_readfirstlane((int)blockIdx.x / p.per_unit);
     index = (int)blockIdx.x - r.unit * p.per_unit;
-    r.n_runs = p.nprobe + (p.resident >= 0 ? 1 : 0);
-    r.n_keys = p.listed ? take_list(p, r.unit, c) : p.rows;
+    r.n_runs = p.listed ? p.nprobe + (p.resident >= 0 ? 1 : 0) : p.unit ? __builtin_amdgcn_readfirstlane(p.unit[r.unit].x) : 0;
+    r.n_keys = p.listed ? take_list(p, r.unit, c) : __builtin_amdgcn_readfirstlane(keys_of_unit(p, r.unit));
     r.of = min(p.per_unit, max((tiles_of_keys(p, r.n_keys) + p.min_tiles - 1) / p.min_tiles, 1));
     if (index == 0 && blockIdx.y == 0 && threadIdx.x == 0) p.start[r.unit] = make_int2(r.unit * p.per_unit, r.of);
     r.there = index < r.of;

@@ -40,7 +40,7 @@ def _rotation(**kw):
     (dict(positions=None), -1), (dict(freqs=None), -1), (dict(S=0), -1), (dict(T=0), -1), (dict(Hq=0), -1), (dict(Hkv=-1), -1), (dict(dtype=2), -1),
     (dict(rot=0), -1), (dict(eps=-1.0), -1), (dict(eps=math.nan), -1), (dict(norm=0), -1), (dict(q_stride=4095), -1), (dict(q_stride=4096 + 4), -1),
     (dict(k_stride=1016), -1), (dict(k_stride=1028, dtype=0), None), (dict(k_stride=1026, dtype=0), -1), (dict(q_weight=ODD), -1),
-    (dict(d=64), -2), (dict(rot=130), -2), (dict(rot=24), -2), (dict(rot=144), -2), (dict(S=1 << 20, T=1 << 12), -2), (dict(Hq=5000, q_stride=640000), -2),
+    (dict(d=64), -2), (dict(rot=130), -2), (dict(rot=24), -2), (dict(rot=144), -2), (dict(S=1 << 20, T=1 << 12), -2), (dict(S=1, T=(1 << 25) + 1), -2), (dict(Hq=5000, q_stride=640000), -2),
 ])
 def test_norm_rotate_refuses(lib, kw, status):
     if status is None:

@@ -237,3 +237,18 @@ def test_captured_and_on_two_streams():
     here = both()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) and torch.equal(a, c) for a, b, c in zip(want, here, there))
+
+
+def test_tokens_far_apart():
+    """Rows 2^30 elements apart, the last one 4 GB and more behind the first: each has the bits that it has in a dense tensor."""
+    g = torch.Generator().manual_seed(31)
+    wide = torch.zeros(1, 4, 2 ** 30, dtype=torch.bfloat16, device=DEV)
+    wide[0, :, :6 * 128] = torch.randn(4, 6 * 128, generator=g).to(torch.bfloat16).to(DEV)
+    q, k = wide[..., :4 * 128].unflatten(2, (4, 128)), wide[..., 4 * 128:6 * 128].unflatten(2, (2, 128))
+    pos, f, w = torch.arange(4, dtype=torch.int32, device=DEV)[None], saap.rotary_frequencies(128, device=DEV), torch.rand(128, generator=g).to(DEV)
+    far, near = saap.norm_rotate(q, k, pos, f, w, w), saap.norm_rotate(q.contiguous(), k.contiguous(), pos, f, w, w)
+    assert all(torch.equal(a, b) for a, b in zip(far, near))
+    grads = [torch.randn(t.shape, generator=g).to(torch.bfloat16).to(DEV) for t in near]
+    names = dict(zip(("g_q_rot", "g_q_feat", "g_k_rot", "g_k_feat"), grads))
+    far, near = (saap.norm_rotate_grads(a, b, pos, f, w, w, **names) for a, b in ((q, k), (q.contiguous(), k.contiguous())))
+    assert all(torch.equal(a, b) for a, b in zip(far, near))
