@@ -83,6 +83,14 @@ template <bool LISTS> __device__ __forceinline__ int row_of_key(const Place& at,
   return __shfl(at.row, key);
 }
 
+// Four codes as bf16 (exact: four significant bits).
+__device__ __forceinline__ u32x2_t bf16_of_codes(unsigned x) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
+  return (u32x2_t){__builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), 0x07060302u),
+                   __builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), 0x07060302u)};
+}
+
 // The operands of a wave.  A tile's rows of K pass through LDS (`stage`): they are read whole, 16 lanes to 256 bytes (read as the
 // product takes them, 32 bytes of each of 32 rows to an instruction, the lines in flight fill the first cache and the rate stays
 // at 4.4 TB/s), and laid down 16 bytes further apart than they are long: 16 lanes that take the same piece of 16 rows meet
@@ -141,25 +149,16 @@ struct Operands {
     if (codes(DRAFTED)) v[i][0] = stream_from<unsigned>(at);
     else v[i] = stream_from<u32x2_t>(at);
   }
-  // and from the stage
-  __device__ __forceinline__ void stage_v(const char* stage, int col, int half, bool drafted) {
+  // and from a stage of bf16 rows
+  __device__ __forceinline__ void stage_v(const char* stage, int col, int half) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const char* at = stage + v_offset(i, col, half, drafted, stage_row(drafted));
-      if (codes(drafted)) v[i][0] = *reinterpret_cast<const unsigned*>(at);
-      else v[i] = *reinterpret_cast<const u32x2_t*>(at);
-    }
+    for (int i = 0; i < 16; ++i) v[i] = *reinterpret_cast<const u32x2_t*>(stage + v_offset(i, col, half, true, stage_row(true)));
   }
-  // codes become bf16 (exact: four significant bits)
+  // codes become bf16
   __device__ __forceinline__ void widen_v(bool drafted) {
     if (!codes(drafted)) return;
-    typedef float f32x2_t __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const f32x2_t a = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[i][0], false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[i][0], true);
-      v[i][0] = __builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), 0x07060302u);
-      v[i][1] = __builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), 0x07060302u);
-    }
+    for (int i = 0; i < 16; ++i) v[i] = bf16_of_codes(v[i][0]);
   }
   // Infinities and NaN among the tile's values (widened) become zeros; the keys that had some, as bits.
   __device__ __forceinline__ unsigned zero_no_numbers() {

@@ -3,7 +3,8 @@
 // Eight waves, RW of which (2, 4 or 8) have 32 rows each and take the same tiles of keys; KW = 8 / RW such groups share out the
 // tiles of a unit.  A group brings RW / 2 tiles, keys and values, into LDS at a time, every wave a part of them: fetched into
 // registers two stages ahead, laid down when the stage before is done with, one barrier to a stage.  64 KB are on their way to a
-// compute unit at any time.
+// compute unit at any time.  Codes are laid down as bf16: every wave widens its part of a tile, not all of it (64 tokens over 128k
+// codes 245 us, every wave for itself 320).
 #include "tree_body.h"
 
 namespace saap {
@@ -88,8 +89,22 @@ tree_rows_kernel(TreeParams p) {
 #pragma unroll
           for (int m = 0; m < kPer; ++m) {
             const int slot = (m * RW + rw) * 64 + ln;  // keys, then values
-            *reinterpret_cast<u32x4_t*>(to + j * kTileBytes + Op::key_of(slot, false) * Op::stage_row(false) + Op::piece_of(slot, false)) =
-                piece[j * kPer + m];
+            char* row = to + j * kTileBytes + Op::key_of(slot, false) * Op::stage_row(true);
+            const u32x4_t x = piece[j * kPer + m];
+            if constexpr (Op::kCodes) {
+              u32x4_t wide[2];
+#pragma unroll
+              for (int i = 0; i < 8; i += 2) {
+                const u32x2_t y = bf16_of_codes(x[i / 2]);
+                wide[i / 4][i % 4] = y[0];
+                wide[i / 4][i % 4 + 1] = y[1];
+              }
+              u32x4_t* at = reinterpret_cast<u32x4_t*>(row + 2 * Op::piece_of(slot, false));
+              at[0] = wide[0];
+              at[1] = wide[1];
+            } else {
+              *reinterpret_cast<u32x4_t*>(row + Op::piece_of(slot, false)) = x;
+            }
           }
         }
       }
@@ -111,13 +126,12 @@ tree_rows_kernel(TreeParams p) {
         if (__ballot(at.word != 0u) == 0ull) continue; // none of the wave's rows attends it
         const char* tile = stage + ((i & 1) * TS + j) * kTileBytes;
         const int ln = this_lane(), col = ln & 31, half = ln >> 5;
-        f32x16_t s = op.scores(tile, col, half, at.drafted);
+        f32x16_t s = op.scores(tile, col, half, true);
         const unsigned attended = weigh<SHAPED>(p, u, w, at, s, s_pos, col, half);
         if (u.vscale != 1.f && !at.drafted)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] *= u.vscale;
-        op.stage_v(tile + kTile * Op::stage_row(at.drafted), col, half, at.drafted);
-        op.widen_v(at.drafted);
+        op.stage_v(tile + kTile * Op::stage_row(true), col, half);
         if (careful || at.drafted) w.marked |= op.zero_no_numbers() & attended;
         op.add(w.o, s);
       }

@@ -249,6 +249,5 @@ def test_tokens_far_apart():
     far, near = saap.norm_rotate(q, k, pos, f, w, w), saap.norm_rotate(q.contiguous(), k.contiguous(), pos, f, w, w)
     assert all(torch.equal(a, b) for a, b in zip(far, near))
     grads = [torch.randn(t.shape, generator=g).to(torch.bfloat16).to(DEV) for t in near]
-    names = dict(zip(("g_q_rot", "g_q_feat", "g_k_rot", "g_k_feat"), grads))
-    far, near = (saap.norm_rotate_grads(a, b, pos, f, w, w, **names) for a, b in ((q, k), (q.contiguous(), k.contiguous())))
+    far, near = (saap.norm_rotate_grads(a, b, pos, f, *grads, w, w) for a, b in ((q, k), (q.contiguous(), k.contiguous())))
     assert all(torch.equal(a, b) for a, b in zip(far, near))
