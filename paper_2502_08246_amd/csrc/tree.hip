@@ -376,7 +376,9 @@ struct Layout {
     // workgroups to a compute unit by their registers' room: two of four waves, or one of eight, or one of fp32
     const int fit = (staged || f32 ? 1 : 2) * device_cus() / blocks;
     shares = fit < 1 ? 1 : fit > kMaxShares ? kMaxShares : fit;
-    min_tiles = staged ? 8 : 2 * kWaves / RW;
+    // Two tiles to a wave at least, so that the second is on its way under the first; one on fp32, whose products of a tile take
+    // longer than its way (5 sequences of up to 4096 keys 19.6 us, with two 24.2).
+    min_tiles = staged ? 8 : (f32 ? 1 : 2) * kWaves / RW;
     // as many shares as there are workgroups at a time, or one to a unit; as many to every unit where they are alike
     grid = shares > units ? shares : (int)units;
     cap = (runs < n_list + 1 ? runs : n_list + 1) + 1;
