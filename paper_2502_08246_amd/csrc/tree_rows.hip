@@ -127,12 +127,15 @@ tree_rows_kernel(TreeParams p) {
         const char* tile = stage + ((i & 1) * TS + j) * kTileBytes;
         const int ln = this_lane(), col = ln & 31, half = ln >> 5;
         f32x16_t s = op.scores(tile, col, half, true);
-        const unsigned attended = weigh<SHAPED>(p, u, w, at, s, s_pos, col, half);
-        if (u.vscale != 1.f && !at.drafted)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] *= u.vscale;
+        // from the weights' exponentials to the products nothing branches, so that the two overlap
         op.stage_v(tile + kTile * Op::stage_row(true), col, half);
-        if (careful || at.drafted) w.marked |= op.zero_no_numbers() & attended;
+        const unsigned no_numbers = careful || at.drafted ? op.zero_no_numbers() : 0u;
+        w.marked |= weigh<SHAPED>(p, u, w, at, s, s_pos, col, half) & no_numbers;
+        if constexpr (Op::kCodes) {
+          const float by = at.drafted ? 1.f : u.vscale;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] *= by;
+        }
         op.add(w.o, s);
       }
       if (i + 1 < stages) {
