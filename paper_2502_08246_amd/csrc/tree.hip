@@ -4,18 +4,20 @@
 // keys, and the T drafted keys behind them as the tree's bits say.  A row attends the members of its token's listed buckets (or
 // every key of a dense cache), scores may be capped (cap tanh(a / cap)), biased by distance and cut at a first position.
 //
-//   1. plan    (lists only) per (sequence, KV head) the union of the tokens' lists, in the order of the runs: first row, place on
-//              the line of the unit's keys, and which tokens list it;
-//   2. attend  the keys of all units, in tiles of 32, lie on one line that is dealt to the workgroups in equal shares.  A wave has
-//              32 rows and walks tiles of keys: S^T = K Q^T and O = P V on the matrix cores, running maximum and sum per row;
-//   3. merge   the shares of every row (log-sum-exp).
-// Bound by memory up to some 200 rows per KV head (4 R d flops per 512-byte key), by the matrix cores beyond.
+//   1. plan    (lists of single tokens, or too long for the lanes of a wave) per (sequence, KV head) the union of the tokens' lists,
+//              in the order of the runs: first row, place on the line of the unit's keys, and which tokens list it;
+//   2. attend  a unit's keys, in tiles of 32, are dealt to its shares, a workgroup each.  A wave has 32 rows and walks tiles of
+//              keys: S^T = K Q^T and O = P V on the matrix cores, running maximum and sum per row;
+//   3. merge   the shares of every row (log-sum-exp): a launch, or, for few rows, the unit's last workgroup.
+// Up to 32 rows to a KV head the kernels are here, and for fp32 caches; more rows of bf16 and codes: tree_rows.hip.
+// Bound by memory up to some 64 rows per KV head (8 sequences of 8 tokens over 32k keys 6.1 TB/s, of 16 tokens 5.8; short calls by
+// the way to the first keys, the partial results and back, 13 us for 1024 of them), by the vector and matrix instructions of a
+// tile beyond.
 //
-// Operands come straight from memory: K: lane (key, half) reads pieces of its key's row.  Scores leave the matrix cores with lane
-// (query, half) holding keys row_of(r, half), and those are taken to be the keys that the lane contributes to the next product, so
-// weights need no exchange; V: lane (n, half) reads features 4n .. 4n+3 of those keys.  In bf16 a weight enters as parts of 8
-// significant bits: three where the output is fp32 (exact), two where it is bf16 (2^-16 of a weight, a 128th of the rounding of
-// the output).  fp32 caches use the fp32 matrix instructions.
+// Scores leave the matrix cores with lane (query, half) holding keys row_of(r, half), and those are taken to be the keys that the
+// lane contributes to the next product, so weights need no exchange; V: lane (n, half) reads features 4n .. 4n+3 of those keys.
+// In bf16 a weight enters as parts of 8 significant bits: three where the output is fp32 (exact), two where it is bf16 (2^-16 of
+// a weight, a 128th of the rounding of the output).  fp32 caches use the fp32 matrix instructions.
 #include "tree_body.h"
 
 namespace saap {
@@ -365,9 +367,9 @@ struct Layout {
   size_t start, unit, table, ml, o, bytes;               // offsets in the workspace
   Layout(long long units, int R, int runs, int n_list, bool f32) {
     const int tiles = (R + kTile - 1) / kTile;
-    // More than 32 rows: the waves with the rows take a tile of keys from LDS, read once for all of them (64 tokens with 4 heads
-    // over 128k keys: every wave for itself 460 us, bound by the second cache).  fp32 products take eight times as long as
-    // their reads, so its waves read for themselves.
+    // More than 32 rows: the waves with the rows take a tile of keys from LDS, read once for all of them (every wave for itself: 64
+    // tokens with 4 heads over 128k keys 460 us instead of 243, bound by the second cache, 8 sequences of 16 over 32k 281 instead
+    // of 185).  fp32 products take eight times as long as their reads, so its waves read for themselves.
     staged = !f32 && tiles > 1;
     const int most = staged ? 8 : 4;
     RW = 1;

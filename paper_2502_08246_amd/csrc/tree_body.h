@@ -9,7 +9,6 @@ typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 
 constexpr int kTile = 32;             // keys of a tile, rows of a wave
 constexpr int kMaxTokens = 64, kMaxUnits = 4096, kMaxShares = 1024;
-constexpr int kPlanThreads = 1024;
 
 struct TreeParams {
   const void *q, *K, *V, *kt, *vt;    // [S,T,Hq,d]; [S,Hkv,rows,d]; drafted [S,Hkv,T,d] or null

@@ -4,7 +4,10 @@
 // tiles of a unit.  A group brings RW / 2 tiles, keys and values, into LDS at a time, every wave a part of them: fetched into
 // registers two stages ahead, laid down when the stage before is done with, one barrier to a stage.  64 KB are on their way to a
 // compute unit at any time.  Codes are laid down as bf16: every wave widens its part of a tile, not all of it (64 tokens over 128k
-// codes 245 us, every wave for itself 320).
+// codes 235 us, every wave for itself 320).
+// Bound by a tile's instructions: 220 of the vector unit, 16 exponentials among them, and 24 products for 32 rows; at two waves to
+// a SIMD their times add up (64 tokens over 128k keys, 256 rows: 243 us, 570 TFLOP/s of the definition's, 850 with the weights'
+// second part).  Two of 8 waves with rows, one tile to a stage: at the rate of memory, 5.8 TB/s, in long bf16 caches.
 #include "tree_body.h"
 
 namespace saap {
