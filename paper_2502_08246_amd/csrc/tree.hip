@@ -276,7 +276,7 @@ tree_attend_kernel(TreeParams p) {
     o.x += other_half(o.x); o.y += other_half(o.y); o.z += other_half(o.z); o.w += other_half(o.w);
     if (half == 0) put_output(p, place_of_row(p, mine.unit, r), col, o, M, L);
     no |= __ballot(no_number(o.x) | no_number(o.y) | no_number(o.z) | no_number(o.w) | no_number(L)) != 0ull;
-    if (no && lane == 0) atomicOr(&s_no[r >> 5], 1u << (r & 31));
+    if (no && L == L && lane == 0) atomicOr(&s_no[r >> 5], 1u << (r & 31));       // L is no number: nor is any output
   }
   __syncthreads();
   for (int r = 0; r < p.R; ++r)
@@ -346,7 +346,7 @@ tree_merge_kernel(TreeParams p) {
     if (tid == 0 && any != 0ull) s_no = 1;
   }
   __syncthreads();
-  if (__builtin_expect(s_no == 0, 1)) return;
+  if (__builtin_expect(s_no == 0 || L != L, 1)) return;  // L is no number (a score is none): nor is any output, as written
   // a list that was taken as it is: once more
   Cursor list;
   const int n_keys = p.listed ? take_list(p, unit, list) : keys_of_unit(p, unit);

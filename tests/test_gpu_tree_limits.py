@@ -198,3 +198,54 @@ def test_sequences_of_a_batch_do_not_change_each_other():
             got, lse = saap.dense_tree_decode_attention(*one, n_keys=n[s:s + 1])
             assert torch.allclose(got[0], eager[0][s], rtol=1e-4, atol=2e-5) and torch.allclose(lse[0], eager[1][s], rtol=1e-5, atol=1e-5)
     assert torch.isfinite(whole[0]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("T", [2, 12, 40])
+@pytest.mark.parametrize("lists", ["none", "shared", "own"])
+def test_queries_of_tokens_that_are_not_there(dtype, T, lists):
+    """A padded batch whose padding is NaN or infinite: those tokens' rows alone are no numbers, also where a value is infinite too."""
+    c = Case(dtype, 2, T, 4, 2, 300, 16, 5, lists, seed=T + 1).cache()
+    c.vt[0, 0, 0, 5] = float("inf")
+    c.tree[:, :T - 1] |= 1
+    c.tree[:, T - 1] = 0
+    c.q[0, T - 1] = float("nan")
+    c.q[1, T - 1, 2] = float("inf")
+    c.q[1, T - 1, 2, ::2] = -float("inf")
+    got, lse = c.run()
+    seen = c.seen[:, :, T - 1].any(-1)                   # [S,Hkv]
+    assert seen.all()
+    assert got[0, T - 1].isnan().all() and lse[0, T - 1].isnan().all()
+    c.q[0, T - 1] = 0
+    c.q[1, T - 1, 2] = 0
+    want, want_lse = c.run()
+    assert torch.equal(got[:, :T - 1], want[:, :T - 1]) and torch.equal(lse[:, :T - 1], want_lse[:, :T - 1])
+    rest = [h for h in range(4) if h != 2]
+    assert torch.equal(got[1, T - 1, rest], want[1, T - 1, rest])
+    c.compare()
+
+
+@pytest.mark.parametrize("T", [1, 3, 20])
+def test_any_run_may_be_the_resident_one(T):
+    """Among the listed ones of some tokens, the first, the last, and where nothing else is listed."""
+    for nprobe in (0, 4, 70):
+        for run in (0, 7, 127):
+            c = Case("bf16", 2, T, 4, 1, 900, 128, nprobe, "own", seed=run).cache()
+            if nprobe:
+                c.sel[0, 0, 0, 1] = run
+                member = torch.zeros(2, T, 1, 128, dtype=torch.bool).scatter_(-1, c.sel.long(), True).transpose(1, 2)
+                c.seen = member.gather(3, c.ids.long()[:, :, None].expand(-1, -1, T, -1))
+            c.seen = c.seen | (c.ids == run)[:, :, None]
+            d = lambda x: x.to(DEV)  # noqa: E731
+            got, lse = saap.tree_decode_attention(d(c.q), c.Kd, c.Vd, c.off, c.ln, d(c.sel), SCALE, d(c.kt), d(c.vt), d(c.tree), resident_run=run,
+                                                  out_dtype=torch.float32)
+            _compare_all(c, got, lse, c.seen)
+
+
+def test_lengths_outside_the_cache_are_cut():
+    c = Case("bf16", 3, 4, 4, 2, 100, seed=4).cache()
+    c.n_keys = torch.tensor([101, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32)
+    got, lse = c.run()
+    c.seen = c.seen.clone()
+    c.seen[2] = False
+    _compare_all(c, got, lse, c.seen)
