@@ -249,3 +249,31 @@ def test_lengths_outside_the_cache_are_cut():
     c.seen = c.seen.clone()
     c.seen[2] = False
     _compare_all(c, got, lse, c.seen)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+def test_few_rows_captured_and_replayed(dtype):
+    """Shares that the last workgroup of a unit adds up: counters are back at zero after every call, on its own and in a graph that
+    replays with other lists, other calls between."""
+    c = Case(dtype, 2, 2, 8, 2, 3000, 64, 20, "shared", (1, 50), seed=5).cache()
+    d = lambda x: x.to(DEV)  # noqa: E731
+    f = saap.tree_decode_attention_fp8 if c.scales else saap.tree_decode_attention
+    sel = d(c.sel)
+    args = (d(c.q), c.Kd, c.Vd, *c.scales, c.off, c.ln, sel, SCALE, d(c.kt), d(c.vt), d(c.tree))
+    call = lambda: f(*args, resident_run=64, out_dtype=torch.float32)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call() + call()
+    for i in range(4):
+        sel.copy_(torch.rand(2, 2, 64, generator=c.g).topk(20, -1).indices.to(torch.int32))
+        graph.replay()
+        eager = call()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], eager[0]) and torch.equal(out[1], eager[1])
+        assert torch.equal(out[2], eager[0]) and torch.equal(out[3], eager[1])
+    c.sel = sel.cpu()
+    member = torch.zeros(2, 2, 64, dtype=torch.bool).scatter_(-1, c.sel.long(), True)
+    seen = member.gather(2, c.ids.long())[:, :, None].expand(-1, -1, 2, -1)
+    _compare_all(c, *eager, seen | (c.kpos < 1) | (c.kpos >= 2950))
