@@ -958,6 +958,9 @@ int32_t saap_dense_tree_decode_attention_fp8(const saap_tree* tree /* host */, c
  *     [0,B), is not stored and sets the flag, the others are stored
  *   resident_ids [S,Hkv,W], n_sink, n_recent: the index of saap_build_windowed_index (B + 1 runs); a push that is refused
  *     leaves its ring slot as it was.  P <= n_recent, unless n_recent = 0.  NULL, 0, 0: an index without a window (B runs).
+ *     While the window fills (positions below n_sink + n_recent) it takes keys in order: a path that does not begin at
+ *     position len[B], and what follows a key that was not stored, adds no such key (the flag is set); keys of later
+ *     positions are stored as ever.
  */
 int32_t saap_append_accepted(const int32_t* bucket_ids, const void* k_tree, const void* v_tree, const int32_t* path,
                              const int32_t* pos_new, const int32_t* off, int32_t* len, int32_t* idx,

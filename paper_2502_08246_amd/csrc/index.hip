@@ -1283,6 +1283,8 @@ extern "C" int32_t saap_recompact_index(const int32_t* off, const int32_t* len, 
 // after the other would do: a token's target is its own bucket, or, in a window, the bucket of the key whose ring slot it takes;
 // of several with one target each takes the slot behind the one before it, and those that find no room are refused (they are the
 // last ones).  Ring slots of up to n_recent consecutive positions are distinct, so no token meets what another one stored.
+// A window that is still filling is its first l[B] slots: it takes the key of the next position only, and none behind one that it
+// has refused, whose slot would stay unwritten among the others.
 // Bound by latency: path -> ids -> lengths and offsets -> rows.
 constexpr int kMaxPath = 64;
 template <typename C, typename T>
@@ -1306,8 +1308,11 @@ append_accepted_kernel(const int32_t* __restrict__ ids, const T* __restrict__ kt
     const bool live = i < count;
     const int id = live ? ids[(size_t)unit * Tn + node] : -1;
     const int first = live && pos_new ? pos_new[s] : 0, pos = !pos_new ? 0x7fffffff : first < 0 || first > 0x7fffffff - i ? -1 : first + i;
+    const bool is_bucket = (unsigned)id < (unsigned)B;
+    const unsigned long long refused = __ballot(live && !is_bucket);
+    const bool next = res_ids && first == l[B] && !(refused & ((1ull << i) - 1ull));
     // -1: refused   0: slot of a window that is still filling   1: ring slot, a key is displaced   2: straight into its bucket
-    const int kind = !live || (unsigned)id >= (unsigned)B ? -1 : !res_ids ? 2 : pos < 0 ? -1 : pos < W ? 0 : n_recent > 0 ? 1 : 2;
+    const int kind = !live || !is_bucket ? -1 : !res_ids ? 2 : pos < 0 ? -1 : pos < W ? (next ? 0 : -1) : n_recent > 0 ? 1 : 2;
     const int res_base = res_ids ? o[B] : 0;
     int slot = -1, dst = -1, target = -1, moved = -1, ring = -1;
     if (kind == 0) {
