@@ -954,8 +954,8 @@ int32_t saap_dense_tree_decode_attention_fp8(const saap_tree* tree /* host */, c
  *   bucket_ids [S,Hkv,T] int32; k_tree, v_tree [S,Hkv,T,d] dtype: of all drafted tokens
  *   path [S,P] int32: the accepted ones in the order of their positions; an entry outside [0,T) ends a path; 0 < P <= 64
  *   pos_new [S] int32: position of a path's first token, the others follow (NULL records -2; not with resident_ids)
- *   off, len, idx, Ksorted, Vsorted, overflow_flag as in saap_append_keys: a key whose bucket is full, or whose id is outside
- *     [0,B), is not stored and sets the flag, the others are stored
+ *   off, len, idx, Ksorted, Vsorted, overflow_flag as in saap_append_keys: a key whose bucket is full, whose id is outside
+ *     [0,B), or whose position is negative or past INT32_MAX, is not stored and sets the flag, the others are stored
  *   resident_ids [S,Hkv,W], n_sink, n_recent: the index of saap_build_windowed_index (B + 1 runs); a push that is refused
  *     leaves its ring slot as it was.  P <= n_recent, unless n_recent = 0.  NULL, 0, 0: an index without a window (B runs).
  *     While the window fills (positions below n_sink + n_recent) it takes keys in order: a path that does not begin at

@@ -1307,12 +1307,13 @@ append_accepted_kernel(const int32_t* __restrict__ ids, const T* __restrict__ kt
     int32_t* rid = res_ids + (size_t)unit * W;
     const bool live = i < count;
     const int id = live ? ids[(size_t)unit * Tn + node] : -1;
-    const int first = live && pos_new ? pos_new[s] : 0, pos = !pos_new ? 0x7fffffff : first < 0 || first > 0x7fffffff - i ? -1 : first + i;
+    // positions below zero, or past the last number, are none, in every kind of index; idx gets -2 for keys without one
+    const int first = live && pos_new ? pos_new[s] : 0, pos = !pos_new ? 0x7fffffff : first > 0x7fffffff - i ? -1 : first + i;
     const bool is_bucket = (unsigned)id < (unsigned)B;
-    const unsigned long long refused = __ballot(live && !is_bucket);
-    const bool next = res_ids && first == l[B] && !(refused & ((1ull << i) - 1ull));
+    const unsigned long long refused = __ballot(live && !is_bucket && pos >= 0);
+    const bool next = res_ids && max(first, 0) == l[B] && !(refused & ((1ull << i) - 1ull));
     // -1: refused   0: slot of a window that is still filling   1: ring slot, a key is displaced   2: straight into its bucket
-    const int kind = !live || !is_bucket ? -1 : !res_ids ? 2 : pos < 0 ? -1 : pos < W ? (next ? 0 : -1) : n_recent > 0 ? 1 : 2;
+    const int kind = !live || !is_bucket || pos < 0 ? -1 : !res_ids ? 2 : pos < W ? (next ? 0 : -1) : n_recent > 0 ? 1 : 2;
     const int res_base = res_ids ? o[B] : 0;
     int slot = -1, dst = -1, target = -1, moved = -1, ring = -1;
     if (kind == 0) {

@@ -1,10 +1,10 @@
-"""append_accepted where some of the accepted tokens are refused: a window that is still filling keeps its keys together.  Bit by bit
-against the calls for single tokens."""
+"""append_accepted where some of the accepted tokens are refused: a window that is still filling keeps its keys together, and positions
+below zero are refused as the calls for single tokens refuse them.  Bit by bit against those calls."""
 import pytest
 import torch
 
 import paper_2502_08246_amd as saap
-from test_gpu_accept import DEV, _index
+from test_gpu_accept import DEV, _index, _one_by_one
 
 pytestmark = pytest.mark.gpu
 NAMES = ("off", "len", "idx", "Ks", "Vs", "resident_ids")
@@ -87,3 +87,19 @@ def test_a_filling_window_takes_the_next_position_only(kind):
             assert torch.equal(a, b), (first, name)
     flag = _accept(ids, k, v, path, torch.tensor([N], dtype=torch.int32, device=DEV), index, scales, window)
     assert int(flag[0]) == 0 and index[1][0, :, 16].tolist() == [N + T] * 2
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "fp8"])
+@pytest.mark.parametrize("window", [None, (0, 0)])
+@pytest.mark.parametrize("first", [-1, -3, -100, 2 ** 31 - 3])
+def test_positions_below_zero_are_refused(first, window, kind):
+    N, T, P = 200, 9, 6
+    cent, index, x, k, v, scales = _start(kind, 2, 2, N, 16, window, T, seed=11)
+    path = torch.tensor([[0, 3, 5, 8, 1, 2], [4, 4, 6, -1, 0, 0]], dtype=torch.int32, device=DEV)
+    pos = torch.tensor([first, N], dtype=torch.int32, device=DEV)
+    theirs = [None if t is None else t.clone() for t in index]
+    want = _one_by_one(theirs, cent, x, k, v, path, pos, window, scales)
+    flag = _accept(saap.assign_keys(x, cent), k, v, path, pos, index, scales, window)
+    assert int(flag[0]) == int(want[0]) == 1
+    for name, a, b in zip(NAMES, index, theirs):
+        assert a is None or torch.equal(a, b), name
