@@ -905,7 +905,8 @@ int32_t saap_norm_rotate_grads(const saap_rotation* rotation /* host */, const v
  *   starts [S,T] int32 or NULL: the first position that a token attends (the begin of its document, or of its span)
  *   out [S,T,Hq,d] of out_dtype;  lse [S,T,Hq] fp32 or NULL
  * An infinity or NaN in a key or value shows in the rows that attend it, where the formula has it, and in no other.  A row that
- * attends one among the values is computed apart, key by key: right, but hundreds of times slower.
+ * attends one among the values, or values so large that 2^8 times their weighted sum leaves fp32, is computed apart, key by key:
+ * right, but hundreds of times slower.  A row whose scores are all -inf ends as one that attends nothing.
  * G in {1,2,4,8}; S*Hkv <= 4096; Ncap < 2^23; B <= SAAP_MAX_BUCKETS.
  * Arithmetic: products of bf16 values are summed in fp32 by the matrix cores; softmax and its sums are in fp32; a weight enters
  * the product with the values in full where out is fp32, with 16 significant bits where it is bf16.  The same inputs give the

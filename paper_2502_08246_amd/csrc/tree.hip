@@ -93,8 +93,9 @@ template <typename C> __device__ __forceinline__ float element(const char* row, 
   else return Vec8<C>::widen(reinterpret_cast<const C*>(row)[e]);
 }
 
-// A row that attends infinities or NaN: computed from the definition, key by key.  Ordinary values never
-// come here.  -> the output's feature `tid` (tid < 128).
+// A row that attends infinities or NaN, or whose weighted sum leaves the range of fp32: computed from the definition, key by key.
+// Ordinary values never come here.  Scores and sums are in double: a bias of far keys is 10^5, of which only differences count, and
+// values near the largest number add up beyond it.  -> the output's feature `tid` (tid < 128).
 template <typename C>
 __device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit, int row, int n_runs, int n_keys, float* s_w /* 256 */,
                                                   float* s_red /* 8 */, const int4* runs /* p.listed */) {
@@ -115,7 +116,8 @@ __device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit
     in = ((unsigned)(t < 32 ? e.z : e.w) >> (t & 31)) & 1u;
     return min(e.y + key - e.x, p.rows - 1);
   };
-  float M = kNegBig, L = 0.f, acc = 0.f;
+  float M = kNegBig;                                     // reference of the weights: near the highest score
+  double L = 0., acc = 0.;
   for (int base = 0; base < n; base += 256) {
     // a thread to a key
     const int key = base + tid;
@@ -135,21 +137,22 @@ __device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit
       pos = lists ? (p.idx ? p.idx[at] : 0) : r;
       if (p.starts) in = in && pos >= p.starts[token];
     }
-    float a = -INFINITY;
+    double a = -INFINITY;                                // in units of log2
     if (in) {
       const char* k = drafted ? static_cast<const char*>(p.kt) + at * (kD * sizeof(Q)) : static_cast<const char*>(p.K) + at * (kD * sizeof(C));
-      a = 0.f;
-      for (int e = 0; e < kD; ++e) a = fmaf(drafted ? element<Q>(k, e) : element<C>(k, e), element<Q>(q, e), a);
-      a *= p.scale * (p.kscale && !drafted ? p.kscale[unit] : 1.f);
-      if (p.softcap > 0.f) a = capped(a / p.softcap, p.softcap);
-      a *= kLog2e;
-      if (p.slopes) a = fmaf(p.slopes[hq] * kLog2e, (float)(pos - p.pos[token]), a);
+      a = 0.;
+#pragma unroll 8
+      for (int e = 0; e < kD; ++e) a = fma((double)(drafted ? element<Q>(k, e) : element<C>(k, e)), (double)element<Q>(q, e), a);
+      a *= (double)p.scale * (p.kscale && !drafted ? p.kscale[unit] : 1.f);
+      if (p.softcap > 0.f) a = capped((float)a / p.softcap, p.softcap);
+      if (p.slopes) a = fma((double)p.slopes[hq], (double)((long long)pos - p.pos[token]), a);
+      a *= 1.4426950408889634;
     }
-    const float top = wave_max(a);
+    const float top = wave_max((float)a);
     if (lane == 0) s_red[wave] = top;
     __syncthreads();
     const float mn = fmaxf(fmaxf(M, fmaxf(s_red[0], s_red[1])), fmaxf(s_red[2], s_red[3])), alpha = fast_exp2(M - mn);
-    const float w = in ? fast_exp2(a - mn) : 0.f, sum = wave_sum(w);
+    const float w = in ? fast_exp2((float)(a - mn)) : 0.f, sum = wave_sum(w);
     if (lane == 0) s_red[4 + wave] = sum;
     s_w[tid] = in ? w : -1.f;
     __syncthreads();
@@ -161,20 +164,20 @@ __device__ __forceinline__ float row_by_definition(const TreeParams& p, int unit
 #pragma unroll 4
       for (int i = 0; i < min(256, n - base); ++i) {
         const int key_i = base + i;
-        float v;
+        double v;
         if (key_i >= n_keys) {
           v = element<Q>(static_cast<const char*>(p.vt) + ((size_t)unit * p.T + key_i - n_keys) * (kD * sizeof(Q)), tid);
         } else {
           int r = key_i;
           bool in_list;
           if (lists) r = row_of_key(key_i, in_list);
-          v = element<C>(static_cast<const char*>(p.V) + ((size_t)unit * p.rows + r) * (kD * sizeof(C)), tid) * (p.vscale ? p.vscale[unit] : 1.f);
+          v = element<C>(static_cast<const char*>(p.V) + ((size_t)unit * p.rows + r) * (kD * sizeof(C)), tid) * (double)(p.vscale ? p.vscale[unit] : 1.f);
         }
-        acc = s_w[i] < 0.f ? acc : fmaf(s_w[i], v, acc);
+        acc = s_w[i] < 0.f ? acc : fma((double)s_w[i], v, acc);
       }
     __syncthreads();
   }
-  return L == 0.f ? 0.f : acc / L;
+  return L == 0. ? 0.f : (float)(acc / L);
 }
 
 // A row's output, feature 4 c .. 4 c + 3 in lane c of 32, and its lse.
