@@ -876,7 +876,8 @@ int32_t saap_norm_rotate(const saap_rotation* rotation /* host */, const void* q
  *   dx = (u - n mean(u n)) / sqrt(mean(x^2) + eps),  u = g * weight      (norm = 0: dx = g)
  *   g_q_feat, g_q_rot, g_k_feat, g_k_rot: shaped as the outputs; of a given tensor either may be NULL (zero), not both
  *   dq [S,T,Hq,d], dk [S,T,Hkv,d] dtype, out, dense; dq_weight, dk_weight fp32, out, given if and only if the weight is
- * The weights' sums run in fp32 in a fixed order: the same inputs give the same bits.
+ * The weights' sums run in a fixed order, so that the same inputs give the same bits, and in double but for runs of four rows
+ * and one rounding of a workgroup's sum: their error does not grow with the rows.
  * Workspace: SAAP_OP_NORM_ROTATE_GRADS (may be NULL where no weight's gradient is asked for).
  */
 int32_t saap_norm_rotate_grads(const saap_rotation* rotation /* host */, const void* q, const void* k,
