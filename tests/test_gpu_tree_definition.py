@@ -30,6 +30,25 @@ def test_far_keys_and_steep_slopes_beside_a_value_that_is_no_number(dtype, T, li
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
+@pytest.mark.parametrize("lists,window", [("none", None), ("shared", None), ("shared", (1, 40))])
+def test_lists_that_the_last_share_adds_up(dtype, lists, window):
+    """Eight (sequence, head) pairs of eight rows: a list is taken as it is, and the share that ends last has the rows computed apart."""
+    c = Case(dtype, 4, 2, 8, 2, 300, 16, 6, lists, window, seed=8, ragged=lists == "none").cache()
+    c.n_keys = None
+    c.seen = torch.ones_like(c.seen) if lists == "none" else c.seen
+    c.pos = c.pos + 100000
+    slopes = torch.tensor([0.5, 0.25, -0.125, 0.0, 0.5, 0.03, 0.25, 0.01])
+    bad = float("nan") if dtype == "fp8" else float("inf")
+    c.V_held = c.V_held.clone()
+    for s, h in ((0, 0), (0, 1), (2, 1), (3, 0)):
+        n = int(c.seen[s, h, 0].nonzero()[-1])           # the last key that is attended
+        c.Vd[s, h, _slot(c, s, h, n), 77] = 0x7f if dtype == "fp8" else bad
+        c.V_held[s, h, n, 77] = bad
+    c.compare(slopes=slopes)
+    c.compare(torch.bfloat16, slopes=slopes, drafts=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "fp8"])
 @pytest.mark.parametrize("T", [1, 3, 12])
 @pytest.mark.parametrize("lists", ["none", "shared", "own"])
 @pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
