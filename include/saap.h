@@ -848,7 +848,7 @@ int32_t saap_window_push_fp8(const void* x_new, const void* k_new, const void* v
  *   q [S,T,Hq,d], k [S,T,Hkv,d] dtype, tokens q_stride and k_stride elements apart (at least Hq*d, Hkv*d; a multiple of 16
  *     bytes), so that slices of one projection's output can be given; either may be NULL
  *   positions [S,T] int32; freqs [rot/2] DOUBLE (device), in radians per position: the product is taken and reduced in double
- *     precision, so that any position is turned as exactly as the first
+ *     precision (position 2^31 at one radian each: the angle is within 10^-6)
  *   q_weight, k_weight fp32 [d], or [Hq,d] and [Hkv,d] with weight_per_head = 1; or NULL (all ones; NULL if norm = 0)
  *   q_feat, q_rot [S,T,Hq,d] dtype, out (token-major, as the decode calls take queries);
  *   k_feat, k_rot [S,Hkv,T,d] dtype, out (head-major, as assign_keys, build_bucket_index and the trees take keys)

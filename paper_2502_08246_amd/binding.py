@@ -462,7 +462,8 @@ def rotary_frequencies(rot, theta=500000.0, scaling=None, factor=1.0, context=81
 def tree_masks(parents):
     """The masks of tree_decode_attention from the parents of drafted tokens: parents [S,T] (integers; a token's parent comes
     before it, a negative number is the end of the context, T or more a token that is not there) -> int64 [S,T] on its device,
-    bit j of [s,t] set for t itself and its ancestors; 0 for a token that is not there."""
+    bit j of [s,t] set for t itself and its ancestors; 0 for a token that is not there.  Made on the host: parents on a device
+    are waited for, and cannot be given while a stream captures."""
     if parents.dim() != 2 or not 0 < parents.shape[1] <= 64:
         raise ValueError("parents must be [S,T] with up to 64 tokens")
     up = parents.to("cpu", torch.int64)

@@ -1404,7 +1404,8 @@ PyMethodDef methods[] = {
                 "magnitude=1.0, q_features=True, k_features=True, q_rot=None, q_feat=None, k_rot=None, k_feat=None)\n--\n\n"
                 "q [S,T,Hq,d], k [S,T,Hkv,d] (slices of one projection will do; either may be None), positions int32 [S,T], freqs\n"
                 "float64 [rot/2] (rotary_frequencies) -> q_rot, q_feat [S,T,Hq,d], k_rot, k_feat [S,Hkv,T,d]: the heads' norm with fp32\n"
-                "weights [d] or [heads,d], before (feat) and after (rot) the rotation of the first rot features; None where there is none."),
+                "weights [d] or [heads,d], before (feat) and after (rot) the rotation of the first rot features; None where there is none.\n"
+                "The results have no autograd graph: norm_rotate_grads gives the gradients."),
     SAAP_METHOD(norm_rotate_grads,
                 "norm_rotate_grads(q, k, positions, freqs, g_q_rot, g_q_feat, g_k_rot, g_k_feat, q_weight=None, k_weight=None, "
                 "norm=True, eps=1e-06, pairs=False, magnitude=1.0, ws=None)\n--\n\n"

@@ -6,8 +6,10 @@
 // compute unit at any time.  Codes are laid down as bf16: every wave widens its part of a tile, not all of it (64 tokens over 128k
 // codes 235 us, every wave for itself 320).
 // Bound by a tile's instructions: 220 of the vector unit, 16 exponentials among them, and 24 products for 32 rows; at two waves to
-// a SIMD their times add up (64 tokens over 128k keys, 256 rows: 243 us, 570 TFLOP/s of the definition's, 850 with the weights'
-// second part).  Two of 8 waves with rows, one tile to a stage: at the rate of memory, 5.8 TB/s, in long bf16 caches.
+// a SIMD their times add up: the vector unit is busy for 53 % of the cycles, the matrix unit for 44 % (64 tokens over 128k keys, 256
+// rows: 241 us with the merge once the clock has settled, 570 TFLOP/s of the definition's, 850 with the weights' second part; in the
+// first 30 ms of such work 248 to 320).  Two of 8 waves with rows, one tile to a stage: at the rate of memory, 5.8 TB/s, in long bf16
+// caches.
 #include "tree_body.h"
 
 namespace saap {
